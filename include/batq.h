@@ -41,7 +41,8 @@ typedef enum {
   BATQ_ERR_WORKSPACE = 5,   /* workspace smaller than batq_linear_workspace_bytes  */
   BATQ_ERR_SINGULAR = 6,    /* a transform factor is not invertible                */
   BATQ_ERR_CUDA = 7,        /* a CUDA runtime / driver call failed                 */
-  BATQ_ERR_TIMEOUT = 8      /* a bounded device-side wait ran out                  */
+  BATQ_ERR_TIMEOUT = 8,     /* a bounded device-side wait ran out                  */
+  BATQ_ERR_INDEX = 9        /* a kernel met a page, slot or position outside its table */
 } batq_status;
 
 enum { BATQ_SF_ROWMAJOR = 0, BATQ_SF_MMA = 1 };  /* scale-byte layouts, see batq_sf_bytes */
@@ -49,6 +50,7 @@ enum { BATQ_F32 = 0, BATQ_BF16 = 1 };            /* output dtypes of the GEMM   
 
 typedef struct batq_transform batq_transform; /* Theta of one layer: factors + clip ratios */
 typedef struct batq_weight batq_weight;       /* one prepared (transformed, quantized) W   */
+typedef struct batq_kv_cache batq_kv_cache;   /* one layer's paged 8-bit key/value cache   */
 
 const char* batq_status_string(batq_status s);
 int batq_version(void);
@@ -75,6 +77,11 @@ batq_status batq_transform_create(batq_transform** out, int32_t n, int32_t gr, i
                                   const float* right, int64_t right_stride,
                                   const float* clip_lo, const float* clip_hi);
 batq_status batq_transform_destroy(batq_transform* t);
+/* The dual P^-T = diag(P_1^-T..P_k^-T) of a transform, without clip: what the queries go through where the
+ * keys go through P, so that (q P^-T)(k P)^T = q k^T (Sec. 3.2's head-by-head key transform).  The factors'
+ * inverses are computed in fp64 and rounded to fp32.  A handle of its own, on t's device, which must be
+ * current; destroyed with batq_transform_destroy.  SINGULAR if a factor has no inverse. */
+batq_status batq_transform_create_dual(batq_transform** out, const batq_transform* t);
 
 /* Emulation of a BF16 implementation of the transform (Sec. 3.2 keeps the pre-quantization
  * transforms in BF16; Algorithm 1 is two contractions, each of which then stores a bf16 tensor).
@@ -290,8 +297,81 @@ batq_status batq_linear_w4a4_noalloc(const batq_transform* t, const batq_weight*
                                      const void* x_bf16, int64_t s, int64_t ld, void* y,
                                      int32_t y_dtype, int64_t ldy, void* stream);
 
+/* A paged key/value cache of one layer in MXFP8 (the KV8 configurations: E4M3 codes, one E8M0 scale per token,
+ * head and 32 channels, as batq_quantize_act_mxfp8 writes them): the handle names four dev buffers of the caller's,
+ *   k_codes, v_codes    [pages][kv_heads][page_size][head_dim] bytes,
+ *   k_scales, v_scales  [pages][kv_heads][page_size][head_dim / 32] bytes,
+ * dense, 16-byte aligned, which outlive it.  Nothing is allocated on the device and nothing is written: several
+ * handles may name the same buffers.  Slot s is token s % page_size of page s / page_size.
+ *   page_size 16, 32, 64 or 128; head_dim 64 or 128 (else UNSUPPORTED); pages * kv_heads * page_size < 2^31 (else
+ *   SHAPE). */
+batq_status batq_kv_cache_create(batq_kv_cache** out, void* k_codes, void* k_scales, void* v_codes, void* v_scales,
+                                 int64_t pages, int32_t page_size, int32_t kv_heads, int32_t head_dim);
+batq_status batq_kv_cache_destroy(batq_kv_cache* c);
+
+/* New tokens into the cache, and their queries through the same rotation, in one launch.  With x = (x_1, x_2) the
+ * halves of the first rot_dim channels of a head and (cos, sin) its token's row of the table,
+ *   rope(x) = (x_1 cos - x_2 sin, x_2 cos + x_1 sin, the other channels as they are);
+ *   keys     MXFP8(clip(rope(k) P_k)),  values  MXFP8(clip(v P_v))   to the token's slot,
+ *   queries  bf16(rope(q) P_q)                                       to q_out,
+ * in fp32 from the bf16 input to the one rounding.
+ *   t_k, t_v, t_q  transforms with n = head_dim, or NULL (none); t_q as batq_transform_create_dual(t_k) makes it, with
+ *                  no clip (else UNSUPPORTED).  UNSUPPORTED while one emulates bf16 intermediates.
+ *   k, v           dev bf16 [tokens x kv_heads * head_dim], row strides ldk, ldv elements: e.g. column ranges of the
+ *                  output of the qkv projection.
+ *   slots          dev int64 [tokens]: where each token goes.  A negative slot marks a padding row: nothing of it is
+ *                  read or written, its row of q_out is left as it was.  The others must differ from one another (a
+ *                  slot given twice holds a mixture of the two tokens).
+ *   positions      dev int32 [tokens]: the token's row of the table; NULL: row i for token i (a table gathered per
+ *                  token, as a rotation with several position components needs it).
+ *   rope           dev fp32 [rope_rows x rot_dim], rot_dim / 2 cosines then rot_dim / 2 sines per row, 16-byte
+ *                  aligned; NULL: no rotation (rot_dim, rope_rows and positions are not looked at).
+ *   rot_dim        a multiple of 16, 16 <= rot_dim <= head_dim.
+ *   q, q_out       dev bf16 [tokens x q_heads * head_dim], strides ldq, ldqo, or both NULL; q_out may be q.
+ * A slot outside the pool or a position outside the table: the token's rows are left out and the next
+ * batq_last_device_status returns BATQ_ERR_INDEX.  tokens == 0 is a no-op.  All of q, k, v 16-byte aligned, strides
+ * multiples of 8.  No workspace; capturable; calls that write different slots may run at the same time. */
+batq_status batq_kv_append_mxfp8(const batq_kv_cache* c, const batq_transform* t_k, const batq_transform* t_v,
+                                 const batq_transform* t_q, const void* k_bf16, int64_t ldk, const void* v_bf16,
+                                 int64_t ldv, const void* q_bf16, int64_t ldq, void* q_out, int64_t ldqo, int32_t q_heads,
+                                 int64_t tokens, const int64_t* slots, const int32_t* positions, const float* rope,
+                                 int64_t rope_rows, int32_t rot_dim, void* stream);
+
+/* Attention of a batch of sequences over the cache.  Sequence i has the query rows q_starts[i] .. q_starts[i+1] - 1
+ * and kv_lens[i] keys, the last of which belong to these rows: with n rows and len keys, row j sees the keys
+ * 0 .. len - n + j when causal, all len otherwise.  For each query head h, with kv head h / (q_heads / kv_heads),
+ *   out = sum_t p_t v_t,   p = softmax(scale * q . k),   lse = log sum_t exp(scale * q . k_t),
+ * k and v as the codes and scales stand for them.  A row that sees no key gets out = 0, lse = -infinity.
+ *   q, out       dev bf16 [tokens x q_heads * head_dim], row strides ldq, ldo; q 16-byte aligned with ldq % 8 == 0,
+ *                out likewise; out may not be q.
+ *   q_heads      a multiple of the cache's kv_heads.
+ *   q_starts     dev int32 [seqs + 1], not decreasing, or NULL: one row per sequence, tokens == seqs (else SHAPE).
+ *                Rows of out and lse that belong to no sequence are left as they were.
+ *   kv_lens      dev int32 [seqs].
+ *   page_table   dev int32 [seqs x ld_pages]: the pages of each sequence in the order of its tokens.  Entries behind
+ *                a sequence's last page are not read.  A page outside the pool: its keys are left out and the next
+ *                batq_last_device_status returns BATQ_ERR_INDEX.
+ *   max_q        no sequence has more query rows; max_kv: none has more keys.  Bounds that size the grid and the
+ *                workspace (a captured call is replayed with other lengths within them); what a sequence has beyond
+ *                them, or beyond ld_pages * page_size keys, is not looked at.
+ *   lse          dev fp32 [tokens x q_heads] or NULL.
+ *   workspace    dev, batq_attention_kv_mxfp8_workspace_bytes(...) bytes with the same sizes (may be 0), 256-byte
+ *                aligned; contents need not be initialised; calls sharing it must be ordered on one stream.
+ * The result of a row is the same whenever its call's sizes (seqs, max_q, max_kv, heads) are: nothing depends on the order in which
+ * parts finish.  Finite q, keys and values; values within one block of 32 tokens that are more than 2^28 smaller
+ * than its largest may be taken as 0.  seqs == 0 or tokens == 0 is a no-op.
+ * Errors: NULL / SHAPE / ALIGN / UNSUPPORTED / WORKSPACE / CUDA. */
+size_t batq_attention_kv_mxfp8_workspace_bytes(const batq_kv_cache* c, int32_t q_heads, int64_t tokens, int32_t seqs,
+                                               int32_t max_q, int32_t max_kv);
+batq_status batq_attention_kv_mxfp8(const batq_kv_cache* c, const void* q_bf16, int64_t ldq, int32_t q_heads, int64_t tokens,
+                                    const int32_t* q_starts, const int32_t* kv_lens, const int32_t* page_table,
+                                    int64_t ld_pages, int32_t seqs, int32_t max_q, int32_t max_kv, float scale, int32_t causal,
+                                    void* out_bf16, int64_t ldo, float* lse, void* workspace, size_t workspace_bytes,
+                                    void* stream);
+
 /* Synchronises `stream` and returns BATQ_ERR_TIMEOUT if any kernel of this
- * library gave up a bounded wait since the last query (the record is cleared),
+ * library gave up a bounded wait since the last query, BATQ_ERR_INDEX if one met an
+ * index outside its table (the record is cleared),
  * BATQ_ERR_CUDA if the stream reports an error, else BATQ_OK. */
 batq_status batq_last_device_status(void* stream);
 

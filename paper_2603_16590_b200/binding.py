@@ -20,7 +20,7 @@ BATQ_OK = 0
 SF_ROWMAJOR, SF_MMA = 0, 1
 F32, BF16 = 0, 1
 STATUS_NAMES = {0: "OK", 1: "ERR_NULL", 2: "ERR_SHAPE", 3: "ERR_ALIGN", 4: "ERR_UNSUPPORTED",
-                5: "ERR_WORKSPACE", 6: "ERR_SINGULAR", 7: "ERR_CUDA", 8: "ERR_TIMEOUT"}
+                5: "ERR_WORKSPACE", 6: "ERR_SINGULAR", 7: "ERR_CUDA", 8: "ERR_TIMEOUT", 9: "ERR_INDEX"}
 
 _LIB = None
 _CALL = None     # csrc/pycall.c: the calls a program makes per layer, without ctypes' conversions
@@ -33,6 +33,7 @@ SIGNATURES = {
     "batq_version": (C.c_int, []),
     "batq_transform_create": (C.c_int, [C.POINTER(_P), _I32, _I32, _I32, _P, _I64, _P, _I64, _P, _P]),
     "batq_transform_destroy": (C.c_int, [_P]),
+    "batq_transform_create_dual": (C.c_int, [C.POINTER(_P), _P]),
     "batq_transform_set_bf16_intermediates": (C.c_int, [_P, _I32]),
     "batq_sf_bytes": (_SZ, [_I64, _I64, _I32]),
     "batq_quantize_act": (C.c_int, [_P, _P, _I64, _I64, _I64, _P, _P, _I32, _P]),
@@ -69,6 +70,12 @@ SIGNATURES = {
     "batq_host_drain": (C.c_int, [_P]),
     "batq_static_workspace_capacity": (_SZ, []),
     "batq_linear_w4a4_noalloc": (C.c_int, [_P, _P, _P, _I64, _I64, _P, _I32, _I64, _P]),
+    "batq_kv_cache_create": (C.c_int, [C.POINTER(_P), _P, _P, _P, _P, _I64, _I32, _I32, _I32]),
+    "batq_kv_cache_destroy": (C.c_int, [_P]),
+    "batq_kv_append_mxfp8": (C.c_int, [_P, _P, _P, _P, _P, _I64, _P, _I64, _P, _I64, _P, _I64, _I32, _I64, _P, _P, _P, _I64, _I32, _P]),
+    "batq_attention_kv_mxfp8_workspace_bytes": (_SZ, [_P, _I32, _I64, _I32, _I32, _I32]),
+    "batq_attention_kv_mxfp8": (C.c_int, [_P, _P, _I64, _I32, _I64, _P, _P, _P, _I64, _I32, _I32, _I32, C.c_float, _I32, _P, _I64, _P,
+                                          _P, _SZ, _P]),
     "batq_last_device_status": (C.c_int, [_P]),
     "batq_debug_wait_timeout": (C.c_int, [_I64, _P]),
     "batq_debug_wait_received_timeout": (C.c_int, [_I64, _P]),
@@ -206,6 +213,15 @@ class Transform:
 
 def batq_transform_create(n, left, right, clip_lo=None, clip_hi=None, gr=4, gc=8) -> Transform:
     return Transform(n, left, right, clip_lo, clip_hi, gr, gc)
+
+
+def batq_transform_create_dual(t: Transform) -> Transform:
+    """P^-T of a transform, without clip: for the queries where the keys go through P."""
+    h = _P()
+    _check(load().batq_transform_create_dual(C.byref(h), t.handle), "batq_transform_create_dual")
+    dual = Transform.__new__(Transform)
+    dual._keep, dual.handle, dual.n = (), h, t.n
+    return dual
 
 
 def batq_transform_set_bf16_intermediates(t: Transform, on: bool):
@@ -404,6 +420,66 @@ def batq_debug_gemm_choice(s, m, n, mxfp8=False, sm_count=148):
 
 def batq_linear_kernel_launches(t, w: Weight, s) -> int:
     return load().batq_linear_kernel_launches(t.handle if t is not None else None, w.handle, s)
+
+
+class KVCache:
+    """Owns a batq_kv_cache handle and keeps the four buffers behind it."""
+
+    def __init__(self, k_codes, k_scales, v_codes, v_scales):
+        pages, heads, page_size, d = k_codes.shape
+        for x, last in ((k_codes, d), (k_scales, d // 32), (v_codes, d), (v_scales, d // 32)):
+            if x.dtype != torch.uint8 or not x.is_contiguous() or tuple(x.shape) != (pages, heads, page_size, last):
+                raise ValueError("batq_kv_cache_create: dense uint8 buffers, codes [pages, kv_heads, page_size, head_dim] and "
+                                 "scales [pages, kv_heads, page_size, head_dim / 32]")
+        h = _P()
+        _check(load().batq_kv_cache_create(C.byref(h), _ptr(k_codes), _ptr(k_scales), _ptr(v_codes), _ptr(v_scales), pages, page_size,
+                                           heads, d), "batq_kv_cache_create")
+        self.k_codes, self.k_scales, self.v_codes, self.v_scales = k_codes, k_scales, v_codes, v_scales
+        self.handle, self.kv_heads, self.head_dim = h, heads, d
+
+    def close(self):
+        if self.handle:
+            load().batq_kv_cache_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def batq_kv_cache_create(k_codes, k_scales, v_codes, v_scales) -> KVCache:
+    """uint8 CUDA buffers: codes [pages, kv_heads, page_size, head_dim], scales [pages, kv_heads, page_size, head_dim / 32]."""
+    return KVCache(k_codes, k_scales, v_codes, v_scales)
+
+
+def batq_kv_append_mxfp8(cache: KVCache, t_k, t_v, k, v, slots, positions=None, rope=None, t_q=None, q=None, q_out=None):
+    """k, v, q: bf16 [tokens, heads * head_dim] with any row stride; slots int64, positions int32 [tokens]; rope fp32
+    [rows, rot_dim], cosines then sines."""
+    tokens = k.shape[0]
+    with_q = q is not None
+    st = load().batq_kv_append_mxfp8(
+        cache.handle, t_k.handle if t_k else None, t_v.handle if t_v else None, t_q.handle if t_q else None, _ptr(k), k.stride(0),
+        _ptr(v), v.stride(0), _ptr(q), q.stride(0) if with_q else 0, _ptr(q_out), q_out.stride(0) if q_out is not None else 0,
+        q.shape[1] // cache.head_dim if with_q else 0, tokens, _ptr(slots), _ptr(positions), _ptr(rope),
+        rope.shape[0] if rope is not None else 0, rope.shape[1] if rope is not None else 0, _stream())
+    _check(st, "batq_kv_append_mxfp8")
+
+
+def batq_attention_kv_mxfp8_workspace_bytes(cache: KVCache, q_heads, tokens, seqs, max_q, max_kv) -> int:
+    return load().batq_attention_kv_mxfp8_workspace_bytes(cache.handle, q_heads, tokens, seqs, max_q, max_kv)
+
+
+def batq_attention_kv_mxfp8(cache: KVCache, q, out, kv_lens, page_table, max_q, max_kv, workspace=None, q_starts=None, scale=None,
+                            causal=True, lse=None):
+    """q, out: bf16 [tokens, q_heads * head_dim] with any row stride; kv_lens int32 [seqs]; page_table int32 [seqs, pages];
+    q_starts int32 [seqs + 1], None: one row per sequence; scale None: head_dim ** -0.5."""
+    st = load().batq_attention_kv_mxfp8(
+        cache.handle, _ptr(q), q.stride(0), q.shape[1] // cache.head_dim, q.shape[0], _ptr(q_starts), _ptr(kv_lens), _ptr(page_table),
+        page_table.stride(0), kv_lens.shape[0], max_q, max_kv, cache.head_dim ** -0.5 if scale is None else scale, 1 if causal else 0,
+        _ptr(out), out.stride(0), _ptr(lse), _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream())
+    _check(st, "batq_attention_kv_mxfp8")
 
 
 def aligned_workspace(nbytes, device="cuda"):

@@ -15,6 +15,7 @@
 #include <new>
 #include <vector>
 
+#include "attention_kv.cuh"
 #include "gemm_mxfp4.cuh"
 #include "gemm_mxfp4_pair.cuh"
 #include "gemm_mxfp4_wide.cuh"
@@ -22,6 +23,7 @@
 #include "gemm_w4a8.cuh"
 #include "gemm_w4a8_pair.cuh"
 #include "gemm_w4a8_wide.cuh"
+#include "kv_append.cuh"
 #include "linear_prefill_fused.cuh"
 #include "linear_small_s_fused.cuh"
 #include "mma_peak.cuh"
@@ -72,6 +74,14 @@ struct batq_weight {
   CUtensorMap tmap_u4_256;  // 128 elements x 128 / 256 weight rows
   CUtensorMap tmap_u4_32;   // 128 elements x 32 weight rows: the W4A8 CTA-pair kernel composes its half tiles from them
   CUtensorMap tmap_sf1;     // scale atoms, boxes of one atom = the 4 blocks of one 128-element K step
+};
+
+struct batq_kv_cache {
+  int device, sm_count;
+  int64_t pages;
+  int32_t page_size, page_shift, kv_heads, head_dim;
+  uint8_t *k_codes, *k_scales, *v_codes, *v_scales;
+  CUtensorMap tmap_k, tmap_v;   // codes as [pages * kv_heads * page_size] rows of head_dim bytes, boxes of 32 rows (16-token pages: 16)
 };
 
 // Scratch for batq_linear_w4a4_noalloc: part of the library image, one copy per GPU.
@@ -184,6 +194,10 @@ batq_status device_setup(int* device_out, const DeviceInfo** info_out) {
     e = e ? e : set_smem(gemm_small_s_kernel<64, true, true>, SmallCfg<64, true>::kSmemBytes);
     e = e ? e : set_smem(gemm_small_s_kernel<128, false, true>, SmallCfg<128, true>::kSmemBytes);
     e = e ? e : set_smem(gemm_small_s_kernel<128, true, true>, SmallCfg<128, true>::kSmemBytes);
+    e = e ? e : set_smem(attention_kv_kernel<128, 1>, AttnCfg<128, 1>::kSmemBytes);
+    e = e ? e : set_smem(attention_kv_kernel<128, 2>, AttnCfg<128, 2>::kSmemBytes);
+    e = e ? e : set_smem(attention_kv_kernel<64, 1>, AttnCfg<64, 1>::kSmemBytes);
+    e = e ? e : set_smem(attention_kv_kernel<64, 2>, AttnCfg<64, 2>::kSmemBytes);
     if (e != cudaSuccess) { cudaGetLastError(); return BATQ_ERR_CUDA; }
     if (g_encode_tiled == nullptr) {
       void* fn = nullptr;
@@ -314,6 +328,18 @@ bool invert_small(const double* a, int n, double* inv) {
   }
   for (int r = 0; r < n; ++r)
     for (int c = 0; c < n; ++c) inv[r * n + c] = w[r * 2 * n + n + c];
+  return true;
+}
+
+// The transposed inverses of `count / (n * n)` matrices, rounded to fp32; false where one has none.
+bool inverse_transposed(const float* a, size_t count, int n, float* out) {
+  std::vector<double> m(static_cast<size_t>(n) * n), inv(m.size());
+  for (size_t at = 0; at < count; at += m.size()) {
+    for (size_t i = 0; i < m.size(); ++i) m[i] = a[at + i];
+    if (!invert_small(m.data(), n, inv.data())) return false;
+    for (int r = 0; r < n; ++r)
+      for (int c = 0; c < n; ++c) out[at + static_cast<size_t>(r) * n + c] = static_cast<float>(inv[static_cast<size_t>(c) * n + r]);
+  }
   return true;
 }
 
@@ -1646,6 +1672,82 @@ batq_status launch_gemm_w4a8(const void* x_codes8, const void* x_sf, const batq_
   return BATQ_OK;
 }
 
+// ------------------------------------------------------------------------------------ key/value cache
+// bf16 rows of `heads` heads: a stride of at least one row, everything 16-byte aligned.
+batq_status check_heads(const void* x, int64_t ld, int64_t heads, int32_t head_dim) {
+  if (x == nullptr) return BATQ_ERR_NULL;
+  if (ld < heads * head_dim || ld > (int64_t(1) << 32)) return BATQ_ERR_SHAPE;
+  return ld % 8 != 0 || !aligned(x, 16) ? BATQ_ERR_ALIGN : BATQ_OK;
+}
+
+batq_status check_kv_transform(const batq_transform* t, const batq_kv_cache* c) {
+  if (t == nullptr) return BATQ_OK;
+  if (t->n != c->head_dim) return BATQ_ERR_SHAPE;
+  if (t->bf16_mid) return BATQ_ERR_UNSUPPORTED;
+  return t->device == c->device ? BATQ_OK : BATQ_ERR_CUDA;
+}
+
+template <int D>
+cudaError_t launch_append(int gc, int grid, const KvAppendParams& p, cudaStream_t stream) {
+  void (*kernel)(const KvAppendParams) = nullptr;
+  switch (gc) {
+    case 0: kernel = kv_append_kernel<D, 0>; break;
+    case 1: kernel = kv_append_kernel<D, 1>; break;
+    case 2: kernel = kv_append_kernel<D, 2>; break;
+    case 4: kernel = kv_append_kernel<D, 4>; break;
+    case 8: kernel = kv_append_kernel<D, 8>; break;
+    case 16: kernel = kv_append_kernel<D, 16>; break;
+    default: kernel = kv_append_kernel<D, 32>; break;
+  }
+  kernel<<<grid, kKvThreads, 0, stream>>>(p);
+  return cudaGetLastError();
+}
+
+// How a call of the attention is cut: rows per CTA, tiles per CTA, CTAs per row tile.
+struct AttnPlan {
+  int nt, row_tiles, chunk, splits;
+  int64_t units;   // (sequence, head, row tile)
+  size_t part_o, part_ml, bytes;
+};
+bool plan_attention(const batq_kv_cache* c, int32_t q_heads, int64_t tokens, int32_t seqs, int32_t max_q, int32_t max_kv, AttnPlan* a) {
+  (void)tokens;
+  const int64_t rows = static_cast<int64_t>(max_q) * (q_heads / c->kv_heads);
+  a->nt = rows <= 8 ? 1 : 2;
+  const int64_t row_tiles = (rows + 8 * a->nt - 1) / (8 * a->nt), units = row_tiles * c->kv_heads * seqs;
+  if (units > (int64_t(1) << 30)) return false;
+  a->row_tiles = static_cast<int>(row_tiles);
+  a->units = units;
+  const int64_t tiles = std::max<int64_t>(1, (static_cast<int64_t>(max_kv) + kAtTile - 1) / kAtTile);
+  const int64_t want = std::max<int64_t>(1, (int64_t(8) * c->sm_count + units - 1) / units);
+  const int64_t chunk = std::max<int64_t>(8, (tiles + want - 1) / want);
+  a->chunk = static_cast<int>(chunk);
+  a->splits = static_cast<int>((tiles + chunk - 1) / chunk);
+  if (units * a->splits > INT_MAX) return false;
+  const size_t parts = a->splits > 1 ? static_cast<size_t>(units) * a->splits * 8 * a->nt : 0;
+  a->part_o = 0;
+  a->part_ml = round_up(parts * c->head_dim * sizeof(float), 256);
+  a->bytes = a->part_ml + round_up(parts * sizeof(float2), 256);
+  return true;
+}
+
+template <int D, int NT>
+cudaError_t launch_attention(const batq_kv_cache* c, const AttnPlan& a, const AttnParams& p, cudaStream_t stream) {
+  attention_kv_kernel<D, NT><<<static_cast<unsigned>(a.units * a.splits), kAtWarps * 32, AttnCfg<D, NT>::kSmemBytes, stream>>>(c->tmap_k, c->tmap_v, p);
+  cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess || a.splits == 1) return e;
+  const int64_t rows = a.units * 8 * NT;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(static_cast<unsigned>((rows + 3) / 4));
+  cfg.blockDim = dim3(128);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, attention_join_kernel<D, NT>, p, rows);
+}
+
 batq_status check_y(const void* y, int32_t y_dtype, int64_t ldy, int64_t m) {
   if (y_dtype != BATQ_F32 && y_dtype != BATQ_BF16) return BATQ_ERR_UNSUPPORTED;
   if (ldy < m) return BATQ_ERR_SHAPE;
@@ -1671,6 +1773,7 @@ const char* batq_status_string(batq_status s) {
     case BATQ_ERR_SINGULAR: return "singular transform factor";
     case BATQ_ERR_CUDA: return "CUDA error";
     case BATQ_ERR_TIMEOUT: return "device-side wait timed out";
+    case BATQ_ERR_INDEX: return "index outside its table";
   }
   return "unknown status";
 }
@@ -1755,6 +1858,21 @@ batq_status batq_transform_destroy(batq_transform* t) {
   cudaFree(t->d_pimg);
   delete t;
   return BATQ_OK;
+}
+
+batq_status batq_transform_create_dual(batq_transform** out, const batq_transform* t) {
+  if (out == nullptr) return BATQ_ERR_NULL;
+  *out = nullptr;
+  if (t == nullptr) return BATQ_ERR_NULL;
+  std::vector<float> left(t->left.size()), right(t->right.size());
+  if (!inverse_transposed(t->left.data(), t->left.size(), t->gr, left.data()) ||
+      !inverse_transposed(t->right.data(), t->right.size(), t->gc, right.data()))
+    return BATQ_ERR_SINGULAR;
+  int dev;
+  batq_status st = device_setup(&dev, nullptr);
+  if (st != BATQ_OK) return st;
+  if (t->device != dev) return BATQ_ERR_CUDA;
+  return batq_transform_create(out, t->n, t->gr, t->gc, left.data(), t->left_stride, right.data(), t->right_stride, nullptr, nullptr);
 }
 
 size_t batq_sf_bytes(int64_t rows, int64_t n, int32_t layout) {
@@ -2457,6 +2575,201 @@ batq_status batq_linear_w4a4_noalloc(const batq_transform* t, const batq_weight*
   return batq_linear_w4a4(t, w, x_bf16, s, ld, y, y_dtype, ldy, ws, batq_static_workspace_capacity(), stream);
 }
 
+batq_status batq_kv_cache_create(batq_kv_cache** out, void* k_codes, void* k_scales, void* v_codes, void* v_scales,
+                                 int64_t pages, int32_t page_size, int32_t kv_heads, int32_t head_dim) {
+  if (out == nullptr) return BATQ_ERR_NULL;
+  *out = nullptr;
+  if (k_codes == nullptr || k_scales == nullptr || v_codes == nullptr || v_scales == nullptr) return BATQ_ERR_NULL;
+  if (pages <= 0 || kv_heads <= 0 || page_size <= 0 || head_dim <= 0) return BATQ_ERR_SHAPE;
+  if ((page_size != 16 && page_size != 32 && page_size != 64 && page_size != 128) || (head_dim != 64 && head_dim != 128))
+    return BATQ_ERR_UNSUPPORTED;
+  if (pages > INT_MAX / page_size / kv_heads) return BATQ_ERR_SHAPE;
+  if (!aligned(k_codes, 16) || !aligned(k_scales, 16) || !aligned(v_codes, 16) || !aligned(v_scales, 16)) return BATQ_ERR_ALIGN;
+  int dev;
+  const DeviceInfo* info;
+  batq_status st = device_setup(&dev, &info);
+  if (st != BATQ_OK) return st;
+  batq_kv_cache* c = new (std::nothrow) batq_kv_cache();
+  if (c == nullptr) return BATQ_ERR_CUDA;
+  c->device = dev;
+  c->sm_count = info->sm_count;
+  c->pages = pages;
+  c->page_size = page_size;
+  for (c->page_shift = 0; (1 << c->page_shift) < page_size; ++c->page_shift) {}
+  c->kv_heads = kv_heads;
+  c->head_dim = head_dim;
+  c->k_codes = static_cast<uint8_t*>(k_codes);
+  c->k_scales = static_cast<uint8_t*>(k_scales);
+  c->v_codes = static_cast<uint8_t*>(v_codes);
+  c->v_scales = static_cast<uint8_t*>(v_scales);
+  const int64_t rows = pages * kv_heads * page_size;
+  const CUtensorMapSwizzle sw = head_dim == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B;
+  const int box = std::min<int>(page_size, kAtTile);
+  st = make_tmap_2d(&c->tmap_k, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, k_codes, head_dim, rows, head_dim, head_dim, box, sw);
+  if (st == BATQ_OK) st = make_tmap_2d(&c->tmap_v, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, v_codes, head_dim, rows, head_dim, head_dim, box, sw);
+  if (st != BATQ_OK) { delete c; return st; }
+  *out = c;
+  return BATQ_OK;
+}
+
+batq_status batq_kv_cache_destroy(batq_kv_cache* c) {
+  delete c;
+  return BATQ_OK;
+}
+
+batq_status batq_kv_append_mxfp8(const batq_kv_cache* c, const batq_transform* t_k, const batq_transform* t_v,
+                                 const batq_transform* t_q, const void* k_bf16, int64_t ldk, const void* v_bf16,
+                                 int64_t ldv, const void* q_bf16, int64_t ldq, void* q_out, int64_t ldqo, int32_t q_heads,
+                                 int64_t tokens, const int64_t* slots, const int32_t* positions, const float* rope,
+                                 int64_t rope_rows, int32_t rot_dim, void* stream) {
+  if (c == nullptr || (q_bf16 == nullptr) != (q_out == nullptr)) return BATQ_ERR_NULL;
+  const bool with_q = q_bf16 != nullptr;
+  if (tokens < 0 || tokens > (int64_t(1) << 30) || (with_q && (q_heads <= 0 || q_heads > (1 << 20)))) return BATQ_ERR_SHAPE;
+  batq_status st = check_kv_transform(t_k, c);
+  if (st == BATQ_OK) st = check_kv_transform(t_v, c);
+  if (st == BATQ_OK) st = check_kv_transform(t_q, c);
+  if (st != BATQ_OK) return st;
+  if (t_q != nullptr && (t_q->has_clip || !with_q)) return BATQ_ERR_UNSUPPORTED;
+  if (rope != nullptr && (rot_dim < 16 || rot_dim > c->head_dim || rot_dim % 16 != 0 || rope_rows <= 0)) return BATQ_ERR_SHAPE;
+  if (rope != nullptr && positions == nullptr && rope_rows < tokens) return BATQ_ERR_SHAPE;
+  if (tokens == 0) return BATQ_OK;
+  if (slots == nullptr) return BATQ_ERR_NULL;
+  st = check_heads(k_bf16, ldk, c->kv_heads, c->head_dim);
+  if (st == BATQ_OK) st = check_heads(v_bf16, ldv, c->kv_heads, c->head_dim);
+  if (st == BATQ_OK && with_q) st = check_heads(q_bf16, ldq, q_heads, c->head_dim);
+  if (st == BATQ_OK && with_q) st = check_heads(q_out, ldqo, q_heads, c->head_dim);
+  if (st != BATQ_OK) return st;
+  if (!aligned(slots, 8) || !aligned(positions, 4) || !aligned(rope, 16)) return BATQ_ERR_ALIGN;
+  int dev;
+  st = device_setup(&dev, nullptr);
+  if (st != BATQ_OK) return st;
+  if (c->device != dev) return BATQ_ERR_CUDA;
+
+  KvAppendParams p{};
+  p.tokens = tokens;
+  p.slots = slots;
+  p.n_slots = c->pages * c->page_size;
+  p.page_shift = c->page_shift;
+  p.rope = rope;
+  p.rope_rows = rope_rows;
+  p.positions = positions;
+  p.rot_dim = rot_dim;
+  const batq_transform* ts[3] = {t_q, t_k, t_v};
+  KvRole roles[3];
+  for (int i = 0; i < 3; ++i) {
+    KvRole& r = roles[i];
+    r = KvRole{};
+    r.x = static_cast<const uint16_t*>(i == 0 ? q_bf16 : i == 1 ? k_bf16 : v_bf16);
+    r.ld = i == 0 ? ldq : i == 1 ? ldk : ldv;
+    r.heads = i == 0 ? q_heads : c->kv_heads;
+    r.rotate = rope != nullptr && i < 2;
+    if (ts[i] != nullptr) {
+      r.xform = 1;
+      r.left = ts[i]->d_left; r.right = ts[i]->d_right;
+      r.left_stride = ts[i]->left_stride; r.right_stride = ts[i]->right_stride;
+      r.clip_lo = ts[i]->d_clip_lo; r.clip_hi = ts[i]->d_clip_hi;
+    }
+    if (i == 0) {
+      r.out = static_cast<uint16_t*>(q_out);
+      r.ldo = ldqo;
+    } else {
+      r.codes = i == 1 ? c->k_codes : c->v_codes;
+      r.scales = i == 1 ? c->k_scales : c->v_scales;
+    }
+  }
+  // One launch for all roles whose transforms have the same factor sizes (those without one join any); usually one.
+  const int rows = kKvThreads / (c->head_dim / 32);
+  bool done[3] = {!with_q, false, false};
+  while (!(done[0] && done[1] && done[2])) {
+    int gc = 0;
+    int64_t grid = 0;
+    for (int i = 0; i < 3; ++i)
+      if (!done[i] && ts[i] != nullptr && gc == 0) gc = ts[i]->gc;
+    for (int i = 0; i < 3; ++i) {
+      p.role[i] = roles[i];
+      const bool now = !done[i] && (ts[i] == nullptr || ts[i]->gc == gc);
+      const int64_t tiles = now ? (tokens * roles[i].heads + rows - 1) / rows : 0;
+      if (tiles > INT_MAX / 4) return BATQ_ERR_SHAPE;
+      p.role[i].tiles = static_cast<int32_t>(tiles);
+      grid += tiles;
+      done[i] = done[i] || now;
+    }
+    const cudaError_t e = c->head_dim == 128 ? launch_append<128>(gc, static_cast<int>(grid), p, static_cast<cudaStream_t>(stream))
+                                             : launch_append<64>(gc, static_cast<int>(grid), p, static_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) return BATQ_ERR_CUDA;
+  }
+  return BATQ_OK;
+}
+
+size_t batq_attention_kv_mxfp8_workspace_bytes(const batq_kv_cache* c, int32_t q_heads, int64_t tokens, int32_t seqs,
+                                               int32_t max_q, int32_t max_kv) {
+  if (c == nullptr || q_heads <= 0 || q_heads % c->kv_heads != 0 || tokens < 0 || seqs < 0 || max_q <= 0 || max_kv < 0) return 0;
+  if (tokens == 0 || seqs == 0) return 0;
+  AttnPlan a;
+  return plan_attention(c, q_heads, tokens, seqs, max_q, max_kv, &a) ? a.bytes : 0;
+}
+
+batq_status batq_attention_kv_mxfp8(const batq_kv_cache* c, const void* q_bf16, int64_t ldq, int32_t q_heads, int64_t tokens,
+                                    const int32_t* q_starts, const int32_t* kv_lens, const int32_t* page_table,
+                                    int64_t ld_pages, int32_t seqs, int32_t max_q, int32_t max_kv, float scale, int32_t causal,
+                                    void* out_bf16, int64_t ldo, float* lse, void* workspace, size_t workspace_bytes,
+                                    void* stream) {
+  if (c == nullptr) return BATQ_ERR_NULL;
+  if (q_heads <= 0 || q_heads % c->kv_heads != 0 || q_heads > (1 << 20) || tokens < 0 || tokens > (int64_t(1) << 30) || seqs < 0 ||
+      max_q <= 0 || max_kv < 0 || ld_pages < 0 || !std::isfinite(scale))
+    return BATQ_ERR_SHAPE;
+  if (q_starts == nullptr && tokens != seqs) return BATQ_ERR_SHAPE;
+  if (seqs == 0 || tokens == 0) return BATQ_OK;
+  if (kv_lens == nullptr || (page_table == nullptr && ld_pages > 0)) return BATQ_ERR_NULL;
+  batq_status st = check_heads(q_bf16, ldq, q_heads, c->head_dim);
+  if (st == BATQ_OK) st = check_heads(out_bf16, ldo, q_heads, c->head_dim);
+  if (st != BATQ_OK) return st;
+  if (!aligned(q_starts, 4) || !aligned(kv_lens, 4) || !aligned(page_table, 4) || !aligned(lse, 4)) return BATQ_ERR_ALIGN;
+  AttnPlan a;
+  if (!plan_attention(c, q_heads, tokens, seqs, max_q, max_kv, &a)) return BATQ_ERR_SHAPE;
+  if (a.bytes > 0) {
+    if (workspace == nullptr) return BATQ_ERR_NULL;
+    if (!aligned(workspace, 256)) return BATQ_ERR_ALIGN;
+    if (workspace_bytes < a.bytes) return BATQ_ERR_WORKSPACE;
+  }
+  int dev;
+  st = device_setup(&dev, nullptr);
+  if (st != BATQ_OK) return st;
+  if (c->device != dev) return BATQ_ERR_CUDA;
+  AttnParams p{};
+  p.q = static_cast<const uint16_t*>(q_bf16);
+  p.ldq = ldq;
+  p.q_heads = q_heads;
+  p.kv_heads = c->kv_heads;
+  p.group = q_heads / c->kv_heads;
+  p.tokens = tokens;
+  p.q_starts = q_starts;
+  p.kv_lens = kv_lens;
+  p.page_table = page_table;
+  p.ld_pages = ld_pages;
+  p.max_q = max_q;
+  p.max_kv = max_kv;
+  p.page_shift = c->page_shift;
+  p.pages = static_cast<int32_t>(c->pages);
+  p.k_scales = c->k_scales;
+  p.v_scales = c->v_scales;
+  p.scale_log2 = static_cast<float>(static_cast<double>(scale) * 1.4426950408889634);
+  p.causal = causal != 0;
+  p.out = static_cast<uint16_t*>(out_bf16);
+  p.ldo = ldo;
+  p.lse = lse;
+  p.row_tiles = a.row_tiles;
+  p.chunk = a.chunk;
+  p.splits = a.splits;
+  p.part_o = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + a.part_o);
+  p.part_ml = reinterpret_cast<float2*>(static_cast<uint8_t*>(workspace) + a.part_ml);
+  const cudaStream_t cs = static_cast<cudaStream_t>(stream);
+  const cudaError_t e = c->head_dim == 128 ? (a.nt == 1 ? launch_attention<128, 1>(c, a, p, cs) : launch_attention<128, 2>(c, a, p, cs))
+                                           : (a.nt == 1 ? launch_attention<64, 1>(c, a, p, cs) : launch_attention<64, 2>(c, a, p, cs));
+  if (e != cudaSuccess) { cudaGetLastError(); return BATQ_ERR_CUDA; }
+  return BATQ_OK;
+}
+
 batq_status batq_last_device_status(void* stream) {
   if (cudaStreamSynchronize(static_cast<cudaStream_t>(stream)) != cudaSuccess) { cudaGetLastError(); return BATQ_ERR_CUDA; }
   int flag = 0;
@@ -2464,7 +2777,7 @@ batq_status batq_last_device_status(void* stream) {
   if (flag != 0) {
     const int zero = 0;
     cudaMemcpyToSymbol(g_device_error, &zero, sizeof(int));
-    return BATQ_ERR_TIMEOUT;
+    return (flag & kErrorTimeout) ? BATQ_ERR_TIMEOUT : BATQ_ERR_INDEX;
   }
   return BATQ_OK;
 }

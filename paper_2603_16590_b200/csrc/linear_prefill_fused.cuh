@@ -110,7 +110,7 @@ __device__ __forceinline__ bool flags_wait_all(const unsigned long long* flags, 
     if (__any_sync(0xFFFFFFFFu, now - t0 > kWaitLimitNs)) {
       if (lane == 0) {
         *abort_flag = 1;
-        atomicExch(&g_device_error, 1);
+        atomicOr(&g_device_error, kErrorTimeout);
       }
       return false;
     }

@@ -6,9 +6,10 @@
 
 namespace batq {
 
-// One word per device: set by a kernel whose bounded wait ran out.  The library
-// is one translation unit, so this definition is the only one.
+// One word per device: set by a kernel whose bounded wait ran out (kErrorTimeout) or that met an index
+// outside its table (kErrorIndex).  The library is one translation unit, so this definition is the only one.
 __device__ int g_device_error = 0;
+constexpr int kErrorTimeout = 1, kErrorIndex = 2;
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) {
   return static_cast<uint32_t>(__cvta_generic_to_shared(p));
@@ -93,7 +94,7 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
     if (t0 == 0) t0 = now;
     if (now - t0 > limit_ns) {
       *abort_flag = 1;
-      atomicExch(&g_device_error, 1);
+      atomicOr(&g_device_error, kErrorTimeout);
       return false;
     }
   }
@@ -251,7 +252,7 @@ __device__ __forceinline__ bool mbar_wait_received(uint32_t bar, volatile int* a
     if (t0 == 0) t0 = now;
     if (now - t0 > limit_ns) {
       *abort_flag = 1;
-      atomicExch(&g_device_error, 1);
+      atomicOr(&g_device_error, kErrorTimeout);
       return false;
     }
   }
