@@ -3,10 +3,15 @@
 //   o = sum_t softmax_t(scale * q . k_t) v_t,   k_t = 2^ek[t,b] kc[t], v_t = 2^ev[t,b] vc[t]   (b: 32-channel block)
 //
 // Bound by the cache's bytes: 33/32 * 2 * head_dim per token and head, read once.  Query rows of one sequence and one
-// key/value head (rows = query rows x heads of the group) share every byte: a CTA takes up to 8 * NT of them and a range
-// of the sequence's tokens.  Its four warps are independent of one another until the end: each has a ring of 32-token
-// tiles filled by TMA, a running maximum and sum, and an accumulator; partial results of warps meet in shared memory,
-// those of CTAs (a long sequence) in the workspace, in a fixed order.
+// key/value head (rows = query rows x heads of the group) share every byte: up to 8 * NT of them are one unit.  The
+// tiles (32 tokens) of all units of the batch stand in one line, cut into ranges of equal cost, one for each CTA that the device
+// holds at once: a ragged batch, one long sequence and many short ones all keep every SM at work to the end.  (A CTA per
+// fixed piece of a sequence instead: 33 against 25 us for 16 sequences of up to 4001 keys, 137 against 58 for one of
+// 131072, 124 against 107 for 128 of up to 8192.)  A cut never falls into a unit of up to kAtSnap tiles; what a cut
+// divides is joined from the workspace, in the order of the tokens, by attention_join_kernel.
+//
+// Within a range a CTA's four warps take every fourth tile and are independent of one another until the unit ends: each
+// has a ring of tiles filled by TMA, a running maximum and sum, and an accumulator; they meet in shared memory.
 //
 // The products run on f16 matrix instructions (m16n8k16, fp32 sums), tokens or channels as the 16 rows and query rows as
 // the 8 columns, because eight query rows would leave half of a 128-row tensor-memory tile's lanes and more unused while
@@ -29,8 +34,19 @@ namespace batq {
 
 constexpr int kAtWarps = 4;
 constexpr int kAtTile = 32;       // tokens a warp takes at a time
-constexpr int kAtStages = 3;
+constexpr int kAtStages = 2;       // x 8.4 KB x 4 warps: three CTAs on an SM
+constexpr int kAtSnap = 8;        // units of up to this many tiles are not divided
+constexpr int kAtMaxSeqs = 512;   // sequences of one launch
+constexpr int kAtUnitCost = 8;    // what a unit costs besides its tiles, in tiles (4 us: look-ups, first loads, the merge)
+constexpr float kAtSlack = 8.0f;  // how far (log2) a score may stand above the reference: weights up to 2^8 in f16
+constexpr float kAtNone = -1e30f; // the reference of a row that has seen no key
 constexpr int kAtMinScale = -32;  // least c: an all-zero tile must not push the softmax sum's terms out of fp32
+
+struct AttnJoin {
+  int32_t parts;     // CTAs that share the unit, this one among them; 0: none starts here
+  int32_t row0, n_rows, head;
+  int64_t q0;        // the sequence's first query row
+};
 
 struct AttnParams {
   const uint16_t* q;          // bf16 bits, row (token, head) at token * ldq + head * head_dim
@@ -51,11 +67,11 @@ struct AttnParams {
   uint16_t* out;              // bf16, row (token, head) at token * ldo + head * head_dim
   int64_t ldo;
   float* lse;                 // [tokens][q_heads] or NULL
-  int32_t row_tiles;          // of a sequence and head, at max_q
-  int32_t chunk;              // tiles of 32 tokens a CTA takes
-  int32_t splits;             // CTAs per row tile, at max_kv
-  float* part_o;              // [unit][split][rows][head_dim]: sums relative to part_ml's reference
-  float2* part_ml;            // [unit][split][rows]: reference exponent m, softmax sum
+  int32_t seqs;               // of this launch, at most kAtMaxSeqs
+  int32_t seq0;               // row of its first sequence where q_starts is NULL
+  float* part_o;              // [CTA][2][rows][head_dim]: sums relative to part_ml's reference
+  float2* part_ml;            // [CTA][2][rows]: reference exponent m, softmax sum
+  AttnJoin* join;             // [CTA]: the unit that starts in its range and ends in another's
 };
 
 template <int D, int NT>
@@ -67,8 +83,10 @@ struct AttnCfg {
   static constexpr int kScaleBytes = kAtTile * kBlocks;            // of K or V
   static constexpr int kRing = kAtWarps * kAtStages * kStageBytes;
   static constexpr int kScales = kAtWarps * kAtStages * 2 * kScaleBytes;
-  static constexpr int kMult = kAtWarps * kBlocks * kAtTile * 2;
-  static constexpr int kSmemBytes = kRing + kScales + kMult + 1024;
+  static constexpr int kMult = kAtWarps * kBlocks * kAtTile * 2;   // 2^(ev - c) of a warp's tile, f16
+  static constexpr int kKeyMult = kAtWarps * kBlocks * kAtTile * 4; // 2^ek, fp32
+  static constexpr int kSmemBytes = kRing + kScales + kMult + kKeyMult + 1024;
+  static constexpr int kCtasPerSm = NT == 1 ? 3 : 2;   // by shared memory; by registers
   static_assert(kAtWarps * kRows * (D + 2) * 4 <= kRing, "the merge of the warps goes through the ring");
 };
 
@@ -80,7 +98,7 @@ struct AttnSeq {
 __device__ __forceinline__ AttnSeq attn_seq(const AttnParams& p, int seq) {
   AttnSeq s;
   if (p.q_starts == nullptr) {
-    s.q0 = seq;
+    s.q0 = p.seq0 + seq;
     s.nq = 1;
   } else {
     const int64_t a = p.q_starts[seq], b = p.q_starts[seq + 1];
@@ -115,6 +133,12 @@ __device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4],
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// The same into fresh accumulators.
+__device__ __forceinline__ void mma_16816_first(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.0f));
 }
 __device__ __forceinline__ void ldmatrix_x4_trans(uint32_t (&r)[4], uint32_t addr) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
@@ -161,414 +185,581 @@ __device__ __forceinline__ void store_attn_row(const AttnParams& p, int64_t toke
   *reinterpret_cast<__nv_bfloat162*>(p.out + token * p.ldo + static_cast<int64_t>(head) * D + ch) = v;
 }
 
+// Tiles of a unit of a sequence with `len` keys (one at least: its rows are written all the same), and its units: the
+// key/value heads times the row tiles.  A row tile counts all of the sequence's tiles, those that its rows do not see too.
+__device__ __forceinline__ int attn_tiles(int len) { return max(1, (len + kAtTile - 1) / kAtTile); }
+template <int NT>
+__device__ __forceinline__ int attn_units(const AttnParams& p, const AttnSeq& s) {
+  return p.kv_heads * ((s.nq * p.group + 8 * NT - 1) / (8 * NT));
+}
+
 template <int D, int NT>
-__global__ void __launch_bounds__(kAtWarps * 32) attention_kv_kernel(const __grid_constant__ CUtensorMap tmap_k,
-                                                                     const __grid_constant__ CUtensorMap tmap_v,
-                                                                     const __grid_constant__ AttnParams p) {
+__global__ void __launch_bounds__(kAtWarps * 32, AttnCfg<D, NT>::kCtasPerSm)
+attention_kv_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
+                    const __grid_constant__ AttnParams p) {
   using Cfg = AttnCfg<D, NT>;
   constexpr int BL = Cfg::kBlocks;
   extern __shared__ __align__(1024) uint8_t at_smem[];
   __shared__ __align__(8) uint64_t bars[kAtWarps * kAtStages];
+  __shared__ int first[kAtMaxSeqs];        // the cost of all units in front of each sequence's
+  __shared__ int weight[kAtMaxSeqs];       // the cost of one of its units: its tiles + kAtUnitCost
+  __shared__ int warp_sum[kAtWarps];
+  __shared__ int2 warp_count[kAtWarps];
   __shared__ int abort_flag;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
   uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(at_smem) + 1023) & ~uintptr_t(1023));
   uint8_t* ring = base + warp * (kAtStages * Cfg::kStageBytes);
   uint8_t* scales = base + Cfg::kRing + warp * (kAtStages * 2 * Cfg::kScaleBytes);
   uint16_t* mult = reinterpret_cast<uint16_t*>(base + Cfg::kRing + Cfg::kScales) + warp * (BL * kAtTile);
+  float* kmult = reinterpret_cast<float*>(base + Cfg::kRing + Cfg::kScales + Cfg::kMult) + warp * (BL * kAtTile);
 
   grid_launch_dependents();
   if (lane == 0) {
     for (int i = 0; i < kAtStages; ++i) mbar_init(smem_u32(&bars[warp * kAtStages + i]), 1);
     mbar_fence_init();
   }
-  if (tid == 0) abort_flag = 0;
-
-  // this CTA's rows and tokens
-  int64_t u = blockIdx.x;
-  const int split = static_cast<int>(u % p.splits);
-  const int64_t unit = u / p.splits;
-  const int rt = static_cast<int>(unit % p.row_tiles);
-  const int head = static_cast<int>(unit / p.row_tiles % p.kv_heads);
-  const int seq = static_cast<int>(unit / p.row_tiles / p.kv_heads);
+  if (tid == 0) {
+    abort_flag = 0;
+    tma_prefetch_desc(&tmap_k);
+    tma_prefetch_desc(&tmap_v);
+  }
   grid_dependency_wait();   // q, the lengths and the cache may come from the grid in front
-  const AttnSeq sq = attn_seq(p, seq);
-  const int row0 = rt * Cfg::kRows, n_rows = min(Cfg::kRows, sq.nq * p.group - row0);
-  if (n_rows <= 0) return;
-  const int end = attn_visible(p, sq, (row0 + n_rows - 1) / p.group);   // keys the last row sees
-  const int tiles = (end + kAtTile - 1) / kAtTile;
-  const int tile0 = split * p.chunk, tile1 = min(tiles, tile0 + p.chunk);
-  if (tile0 >= tiles && split > 0) return;
-  const int used = max(1, (tiles + p.chunk - 1) / p.chunk);             // splits that have tokens
 
-  // q as the matrix instruction's B fragments, scaled by a power of two per row
-  uint32_t qf[NT][BL][4];
-  float qs[NT][2];      // the factor of rows 2 t4, 2 t4 + 1 on the accumulators
-  int lim[NT][2];       // keys those rows see
-#pragma unroll
-  for (int j = 0; j < NT; ++j) {
-    const int row = row0 + j * 8 + g;
-    float v[BL][8];
-    float amax = 0.0f;
-#pragma unroll
-    for (int b = 0; b < BL; ++b) {
-      uint4 w = make_uint4(0u, 0u, 0u, 0u);
-      if (j * 8 + g < n_rows)
-        w = ld_global_ordered_v4(p.q + (sq.q0 + row / p.group) * p.ldq + static_cast<int64_t>(head * p.group + row % p.group) * D + b * 32 + t4 * 8);
-      unpack_bf16x8(w, v[b]);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) amax = fmaxf(amax, fabsf(v[b][i]));
+  // the cost in front of each sequence, and of all; this CTA's range and the sequence that it starts in
+  int pos, stop, seq, chunk;
+  {
+    const int per = (p.seqs + kAtWarps * 32 - 1) / (kAtWarps * 32);
+    const int s0 = min(p.seqs, tid * per), s1 = min(p.seqs, s0 + per);
+    int sum = 0;
+    for (int s = s0; s < s1; ++s) {
+      first[s] = sum;
+      const AttnSeq q = attn_seq(p, s);
+      weight[s] = attn_tiles(q.len) + kAtUnitCost;
+      sum += attn_units<NT>(p, q) * weight[s];
     }
-    amax = fmaxf(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 1));
-    amax = fmaxf(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 2));
-    const int e = max(static_cast<int>(__float_as_uint(amax) >> 23) - 127, -100);
-    const float up = pow2i(14 - e);
+    int scan = sum;
 #pragma unroll
-    for (int b = 0; b < BL; ++b)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const __half2 h = __floats2half2_rn(v[b][2 * i] * up, v[b][2 * i + 1] * up);
-        qf[j][b][i] = *reinterpret_cast<const uint32_t*>(&h);
-      }
-    const float f = p.scale_log2 * pow2i(e - 14);
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      qs[j][i] = __shfl_sync(0xFFFFFFFFu, f, (2 * t4 + i) * 4);
-      const int rr = j * 8 + 2 * t4 + i;
-      lim[j][i] = rr < n_rows ? attn_visible(p, sq, (row0 + rr) / p.group) : 0;
+    for (int x = 1; x < 32; x <<= 1) {
+      const int v = __shfl_up_sync(0xFFFFFFFFu, scan, x);
+      if (lane >= x) scan += v;
     }
-  }
-  const int full = attn_visible(p, sq, row0 / p.group);   // keys that every row sees
-
-  float o[D / 16][NT][4];
-  float m[NT][2], l[NT][2];
-#pragma unroll
-  for (int j = 0; j < NT; ++j) {
-    m[j][0] = m[j][1] = -INFINITY;
-    l[j][0] = l[j][1] = 0.0f;
-#pragma unroll
-    for (int c = 0; c < D / 16; ++c)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) o[c][j][i] = 0.0f;
-  }
-
-  // this warp's tiles: tile0 + warp + 4 i, i < n
-  const int n = tile1 - tile0 > warp ? (tile1 - tile0 - warp + kAtWarps - 1) / kAtWarps : 0;
-  const int32_t* pages = p.page_table + static_cast<int64_t>(seq) * p.ld_pages;
-  const int page_tokens = 1 << p.page_shift;
-  const int parts = page_tokens < kAtTile ? 2 : 1;   // pages of a tile
-  const int part_rows = kAtTile / parts;
-  // The pages of the next 32 tiles to load, one per lane (two for 16-token pages): the look-up is off the tiles' path.
-  int page_a = 0, page_b = 0;
-  auto look_up = [&](int i) {
-    page_a = page_b = -1;
-    if (i + lane < n) {
-      const int tok = (tile0 + warp + kAtWarps * (i + lane)) * kAtTile;
-      page_a = pages[tok >> p.page_shift];
-      if (parts == 2 && tok + part_rows < end) page_b = pages[(tok + part_rows) >> p.page_shift];
-    }
-  };
-  uint32_t bad = 0;   // bits 2 s, 2 s + 1: the first / second part of the tile in stage s is not there
-  auto issue = [&](int i) {
-    if ((i & 31) == 0) look_up(i);
-    const int st = i % kAtStages;
-    const int tok = (tile0 + warp + kAtWarps * i) * kAtTile;
-    int pg[2];
-    pg[0] = __shfl_sync(0xFFFFFFFFu, page_a, i & 31);
-    pg[1] = __shfl_sync(0xFFFFFFFFu, page_b, i & 31);
-    const uint32_t bar = smem_u32(&bars[warp * kAtStages + st]);
-    uint32_t miss = 0;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      if (h >= parts || tok + h * part_rows >= end) continue;
-      if (pg[h] < 0 || pg[h] >= p.pages) {
-        miss |= 1u << h;
-        if (lane == 0) atomicOr(&g_device_error, kErrorIndex);
-      }
-    }
-    bad = (bad & ~(3u << (2 * st))) | (miss << (2 * st));
-    if (lane == 0) {
-      int there = 0;
-      for (int h = 0; h < parts; ++h) there += tok + h * part_rows < end && !((miss >> h) & 1u);
-      mbar_arrive_expect_tx(bar, there * part_rows * 2 * (D + BL));
-      for (int h = 0; h < parts; ++h) {
-        if (tok + h * part_rows >= end || ((miss >> h) & 1u)) continue;
-        const int64_t row = ((static_cast<int64_t>(pg[h]) * p.kv_heads + head) << p.page_shift) + ((tok + h * part_rows) & (page_tokens - 1));
-        const uint32_t dst = smem_u32(ring + st * Cfg::kStageBytes) + h * part_rows * D;
-        tma_load_2d(dst, &tmap_k, 0, static_cast<int32_t>(row), bar);
-        tma_load_2d(dst + Cfg::kCodeBytes, &tmap_v, 0, static_cast<int32_t>(row), bar);
-        const uint32_t sdst = smem_u32(scales + st * 2 * Cfg::kScaleBytes) + h * part_rows * BL;
-        bulk_g2s(sdst, p.k_scales + row * BL, part_rows * BL, bar);
-        bulk_g2s(sdst + Cfg::kScaleBytes, p.v_scales + row * BL, part_rows * BL, bar);
-      }
-    }
-  };
-  __syncthreads();   // abort_flag
-  int issued = 0;
-  for (; issued < kAtStages && issued < n; ++issued) issue(issued);
-
-  const uint32_t mult_addr = smem_u32(mult);
-  bool ok = true;
-  for (int i = 0; i < n; ++i) {
-    const int st = i % kAtStages;
-    const uint32_t bar = smem_u32(&bars[warp * kAtStages + st]);
-    ok = __all_sync(0xFFFFFFFFu, mbar_wait(bar, (i / kAtStages) & 1, &abort_flag));
-    if (!ok) break;
-    const int tok0 = (tile0 + warp + kAtWarps * i) * kAtTile;
-    const uint32_t kt = smem_u32(ring + st * Cfg::kStageBytes), vt = kt + Cfg::kCodeBytes;
-    const uint8_t* ks = scales + st * 2 * Cfg::kScaleBytes;
-    const uint8_t* vs = ks + Cfg::kScaleBytes;
-    const uint32_t miss = (bad >> (2 * st)) & 3u;
-    const bool whole = tok0 + kAtTile <= full && miss == 0;   // every row sees every token
-    const bool here = tok0 + lane < end && !((miss >> (parts == 2 ? lane >> 4 : 0)) & 1u);   // the lane's token
-    if (tok0 + kAtTile > end || miss != 0) {
-      // what stands behind the last token (or on a page that is not there) may be anything, NaN codes too
-      if (!here) {
-#pragma unroll
-        for (int c = 0; c < D / 16; ++c)
-          asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(vt + lane * D + c * 16), "r"(0u) : "memory");
-      }
-    }
-    // the value scales of the lane's token, the tile's common exponent, and the f16 factors 2^(ev - c)
-    int c_tile;
-    {
-      uint32_t w;
-      if (BL == 4) w = *reinterpret_cast<const uint32_t*>(vs + lane * 4);
-      else w = *reinterpret_cast<const uint16_t*>(vs + lane * 2);
-      if (!here) w = 0;
-      int top = 0;
-#pragma unroll
-      for (int b = 0; b < BL; ++b) top = max(top, static_cast<int>((w >> (8 * b)) & 255u));
-      top = __reduce_max_sync(0xFFFFFFFFu, top);
-      c_tile = max(top - 127 - 7, kAtMinScale);
-      const int at = (lane & 24) | token_frag<D>(lane & 7);
-#pragma unroll
-      for (int b = 0; b < BL; ++b) mult[b * kAtTile + at] = static_cast<uint16_t>(f16_pow2(static_cast<int>((w >> (8 * b)) & 255u) - 127 - c_tile));
-    }
-    __syncwarp();
-
-    // S^T [32 tokens x rows] in log2 units, plus c
-    float s[2][NT][4];
-#pragma unroll
-    for (int mt = 0; mt < 2; ++mt) {
-#pragma unroll
-      for (int j = 0; j < NT; ++j)
-#pragma unroll
-        for (int x = 0; x < 4; ++x) s[mt][j][x] = 0.0f;
-      const int ta = mt * 16 + frag_token<D>(g), tb = ta + 8;
-      uint32_t wa, wb;
-      if (BL == 4) {
-        wa = *reinterpret_cast<const uint32_t*>(ks + ta * 4);
-        wb = *reinterpret_cast<const uint32_t*>(ks + tb * 4);
-      } else {
-        wa = *reinterpret_cast<const uint16_t*>(ks + ta * 2);
-        wb = *reinterpret_cast<const uint16_t*>(ks + tb * 2);
-      }
-#pragma unroll
-      for (int b = 0; b < BL; ++b) {
-        uint32_t a0, a1, b0, b1;
-        asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(a0), "=r"(a1) : "r"(kt + tile_offset<D>(ta, 2 * b + (t4 >> 1)) + (t4 & 1) * 8) : "memory");
-        asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(b0), "=r"(b1) : "r"(kt + tile_offset<D>(tb, 2 * b + (t4 >> 1)) + (t4 & 1) * 8) : "memory");
-        const uint32_t f0[4] = {e4m3x2_to_f16x2(a0), e4m3x2_to_f16x2(b0), e4m3x2_to_f16x2_high(a0), e4m3x2_to_f16x2_high(b0)};
-        const uint32_t f1[4] = {e4m3x2_to_f16x2(a1), e4m3x2_to_f16x2(b1), e4m3x2_to_f16x2_high(a1), e4m3x2_to_f16x2_high(b1)};
-        const float ea = __uint_as_float(((wa >> (8 * b)) & 255u) << 23), eb = __uint_as_float(((wb >> (8 * b)) & 255u) << 23);
-#pragma unroll
-        for (int j = 0; j < NT; ++j) {
-          float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-          mma_16816(d, f0, qf[j][b][0], qf[j][b][1]);
-          mma_16816(d, f1, qf[j][b][2], qf[j][b][3]);
-          s[mt][j][0] = fmaf(d[0], ea, s[mt][j][0]);
-          s[mt][j][1] = fmaf(d[1], ea, s[mt][j][1]);
-          s[mt][j][2] = fmaf(d[2], eb, s[mt][j][2]);
-          s[mt][j][3] = fmaf(d[3], eb, s[mt][j][3]);
-        }
-      }
-    }
-    const float cf = static_cast<float>(c_tile);
-#pragma unroll
-    for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-      for (int j = 0; j < NT; ++j)
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          s[mt][j][x] = fmaf(s[mt][j][x], qs[j][x & 1], cf);
-          if (!whole) {
-            const int tt = mt * 16 + (x >> 1) * 8 + frag_token<D>(g);
-            if (tok0 + tt >= lim[j][x & 1] || ((miss >> (parts == 2 ? tt >> 4 : 0)) & 1u)) s[mt][j][x] = -INFINITY;
-          }
-        }
-    // running maximum, weights
-    uint32_t pf[2][NT][2];
-    const float unscale = pow2i(max(-c_tile, -126));
-#pragma unroll
-    for (int j = 0; j < NT; ++j) {
-      float alpha[2], mr[2];
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        float top = fmaxf(fmaxf(s[0][j][x], s[0][j][x + 2]), fmaxf(s[1][j][x], s[1][j][x + 2]));
-        top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 4));
-        top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 8));
-        top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 16));
-        const float mn = fmaxf(m[j][x], top);
-        mr[x] = mn == -INFINITY ? 0.0f : mn;
-        alpha[x] = ex2(m[j][x] - mr[x]);
-        m[j][x] = mn;
-        float sum = 0.0f;
-#pragma unroll
-        for (int mt = 0; mt < 2; ++mt) {
-          s[mt][j][x] = ex2(s[mt][j][x] - mr[x]);
-          s[mt][j][x + 2] = ex2(s[mt][j][x + 2] - mr[x]);
-          sum += s[mt][j][x] + s[mt][j][x + 2];
-        }
-        l[j][x] = fmaf(l[j][x], alpha[x], sum * unscale);
-      }
-#pragma unroll
-      for (int c = 0; c < D / 16; ++c) {
-        o[c][j][0] *= alpha[0];
-        o[c][j][1] *= alpha[1];
-        o[c][j][2] *= alpha[0];
-        o[c][j][3] *= alpha[1];
-      }
-#pragma unroll
-      for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const __half2 w = __floats2half2_rn(s[mt][j][2 * h], s[mt][j][2 * h + 1]);
-          pf[mt][j][h] = movmatrix_trans(*reinterpret_cast<const uint32_t*>(&w));
-        }
-    }
-    // O^T += V^T P^T
-#pragma unroll
-    for (int mt = 0; mt < 2; ++mt) {
-      const int row = mt * 16 + ((lane >> 3) & 1) * 8 + frag_token<D>(lane & 7);
-#pragma unroll
-      for (int b = 0; b < BL; ++b) {
-        uint32_t w[4], s0, s1;
-        ldmatrix_x4_trans(w, vt + tile_offset<D>(row, 2 * b + (lane >> 4)));
-        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(s0) : "r"(mult_addr + (b * kAtTile + mt * 16 + 2 * t4) * 2) : "memory");
-        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(s1) : "r"(mult_addr + (b * kAtTile + mt * 16 + 8 + 2 * t4) * 2) : "memory");
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const uint32_t u0 = __byte_perm(w[2 * c], 0u, 0x3120), u1 = __byte_perm(w[2 * c + 1], 0u, 0x3120);
-          const uint32_t f[4] = {hmul2(e4m3x2_to_f16x2(u0), s0), hmul2(e4m3x2_to_f16x2_high(u0), s0),
-                                 hmul2(e4m3x2_to_f16x2(u1), s1), hmul2(e4m3x2_to_f16x2_high(u1), s1)};
-#pragma unroll
-          for (int j = 0; j < NT; ++j) mma_16816(o[2 * b + c][j], f, pf[mt][j][0], pf[mt][j][1]);
-        }
-      }
-    }
-    __syncwarp();   // every lane is done with the stage
-    if (issued < n) {
-      if (tok0 + kAtTile > end || miss != 0) fence_proxy_async_smem();
-      issue(issued);
-      ++issued;
-    }
-  }
-  if (!ok) {   // given up: copies already in flight land before the CTA leaves
-    for (int i = max(0, issued - kAtStages); i < issued; ++i) {
-      const uint32_t bar = smem_u32(&bars[warp * kAtStages + i % kAtStages]);
-      const uint64_t t0 = global_timer_ns();
-      while (!mbar_try_wait(bar, (i / kAtStages) & 1) && global_timer_ns() - t0 < 100000000ull) {}
-    }
-  }
-#pragma unroll
-  for (int j = 0; j < NT; ++j)
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      l[j][x] += __shfl_xor_sync(0xFFFFFFFFu, l[j][x], 4);
-      l[j][x] += __shfl_xor_sync(0xFFFFFFFFu, l[j][x], 8);
-      l[j][x] += __shfl_xor_sync(0xFFFFFFFFu, l[j][x], 16);
-    }
-  // the warps' results meet in the ring: [warp][row][D], then [warp][row] of (m, l)
-  __syncthreads();
-  float* mo = reinterpret_cast<float*>(base);
-  float2* mm = reinterpret_cast<float2*>(mo + kAtWarps * Cfg::kRows * D);
-#pragma unroll
-  for (int j = 0; j < NT; ++j) {
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const int row = j * 8 + 2 * t4 + x;
-      if (g == 0) mm[warp * Cfg::kRows + row] = make_float2(m[j][x], l[j][x]);
-#pragma unroll
-      for (int c = 0; c < D / 16; ++c)
-        *reinterpret_cast<float2*>(mo + (warp * Cfg::kRows + row) * D + c * 16 + 2 * g) = make_float2(o[c][j][x], o[c][j][x + 2]);
-    }
-  }
-  __syncthreads();
-  const int64_t part = unit * p.splits + split;
-  for (int i = tid; i < n_rows * (D / 2); i += kAtWarps * 32) {
-    const int row = i / (D / 2), ch = (i % (D / 2)) * 2;
-    float top = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < kAtWarps; ++w) top = fmaxf(top, mm[w * Cfg::kRows + row].x);
-    float sum = 0.0f, a = 0.0f, b = 0.0f;
+    if (lane == 31) warp_sum[warp] = scan;
+    __syncthreads();
+    int before = scan - sum, total = 0;
 #pragma unroll
     for (int w = 0; w < kAtWarps; ++w) {
-      const float2 ml = mm[w * Cfg::kRows + row];
-      const float f = ml.x == -INFINITY ? 0.0f : ex2(ml.x - top);
-      const float2 v = *reinterpret_cast<const float2*>(mo + (w * Cfg::kRows + row) * D + ch);
-      sum = fmaf(ml.y, f, sum);
-      a = fmaf(v.x, f, a);
-      b = fmaf(v.y, f, b);
+      if (w < warp) before += warp_sum[w];
+      total += warp_sum[w];
     }
-    if (used == 1) {
-      const int64_t token = sq.q0 + (row0 + row) / p.group;
-      const int qh = head * p.group + (row0 + row) % p.group;
-      const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
-      store_attn_row(p, token, qh, D, ch, a * inv, b * inv);
-      if (ch == 0 && p.lse != nullptr) p.lse[token * p.q_heads + qh] = sum > 0.0f ? (top + log2f(sum)) * 0.69314718055994531f : -INFINITY;
-    } else {
-      *reinterpret_cast<float2*>(p.part_o + (part * Cfg::kRows + row) * D + ch) = make_float2(a, b);
-      if (ch == 0) p.part_ml[part * Cfg::kRows + row] = make_float2(top, sum);
+    chunk = max(kAtWarps, static_cast<int>((static_cast<uint32_t>(total) + gridDim.x - 1) / gridDim.x));
+    const int64_t x0 = static_cast<int64_t>(chunk) * blockIdx.x, x1 = x0 + chunk;
+    int2 n = make_int2(0, 0);   // sequences that start at or before x0, x1
+    for (int s = s0; s < s1; ++s) {
+      const int f = first[s] + before;
+      first[s] = f;
+      n.x += f <= x0;
+      n.y += f <= x1;
     }
+    n.x = __reduce_add_sync(0xFFFFFFFFu, n.x);
+    n.y = __reduce_add_sync(0xFFFFFFFFu, n.y);
+    if (lane == 0) warp_count[warp] = n;
+    __syncthreads();
+    n = make_int2(0, 0);
+#pragma unroll
+    for (int w = 0; w < kAtWarps; ++w) {
+      n.x += warp_count[w].x;
+      n.y += warp_count[w].y;
+    }
+    // A cut stays where it is in a long unit behind what the unit costs before its first tile, else it goes back to the
+    // start of the unit.  (The last sequence that starts at or before it has rows: those without start where the next does.)
+    auto cut = [&](int64_t x, int s) {
+      if (x >= total) return total;
+      const int w = weight[s], in = (static_cast<int>(x) - first[s]) % w;
+      return static_cast<int>(x) - (w <= kAtSnap + kAtUnitCost || in <= kAtUnitCost ? in : 0);
+    };
+    seq = n.x - 1;
+    pos = cut(x0, n.x - 1);
+    stop = cut(x1, n.y - 1);
   }
+  AttnJoin join{};
+  bool ok = true;
+  int turn = 0;             // tiles this warp has taken, over all units
+
+  while (pos < stop) {
+    AttnSeq sq = attn_seq(p, seq);
+    while (pos >= first[seq] + attn_units<NT>(p, sq) * weight[seq]) sq = attn_seq(p, ++seq);   // the next one with rows
+    const int unit = (pos - first[seq]) / weight[seq], unit_tiles = weight[seq] - kAtUnitCost;
+    const int unit0 = first[seq] + unit * weight[seq] + kAtUnitCost;   // its first tile
+    const int tile0 = max(0, pos - unit0), tile1 = min(unit_tiles, stop - unit0);
+    pos = unit0 + tile1;
+    const int head = unit % p.kv_heads, row0 = unit / p.kv_heads * Cfg::kRows;
+    const int n_rows = min(Cfg::kRows, sq.nq * p.group - row0);
+    const int end = attn_visible(p, sq, (row0 + n_rows - 1) / p.group);   // keys the last row sees
+
+    if (end <= 0 && unit_tiles == 1) {   // nothing to see, nothing to join
+      for (int i = tid; i < n_rows * (D / 2); i += kAtWarps * 32) {
+        const int row = row0 + i / (D / 2), ch = i % (D / 2) * 2;
+        const int64_t token = sq.q0 + row / p.group;
+        const int qh = head * p.group + row % p.group;
+        store_attn_row(p, token, qh, D, ch, 0.0f, 0.0f);
+        if (ch == 0 && p.lse != nullptr) p.lse[token * p.q_heads + qh] = -INFINITY;
+      }
+      continue;
+    }
+
+    // this warp's tiles: tile0 + warp + 4 i, i < n
+    const int last = min(tile1, (end + kAtTile - 1) / kAtTile);
+    const int n = ok && last - tile0 > warp ? (last - tile0 - warp + kAtWarps - 1) / kAtWarps : 0;
+    const int32_t* pages = p.page_table + static_cast<int64_t>(seq) * p.ld_pages;
+    const int parts = p.page_shift == 4 ? 2 : 1;   // pages of a tile
+    // The pages of the next 32 tiles to load, one per lane (two for 16-token pages): the look-up is off the tiles' path.
+    int page_a = 0, page_b = 0;
+    auto look_up = [&](int i) {
+      page_a = page_b = -1;
+      if (i + lane < n) {
+        const int tok = (tile0 + warp + kAtWarps * (i + lane)) * kAtTile;
+        page_a = pages[tok >> p.page_shift];
+        if (parts == 2 && tok + 16 < end) page_b = pages[(tok >> 4) + 1];
+      }
+    };
+    // One page's part of a tile: `rows` tokens from token `off` of the page, to row `at` of stage st.
+    auto load = [&](int st, int page, int off, int rows, int at) {
+      const int row = ((page * p.kv_heads + head) << p.page_shift) + off;   // below 2^31
+      const uint32_t bar = smem_u32(&bars[warp * kAtStages + st]);
+      const uint32_t dst = smem_u32(ring + st * Cfg::kStageBytes) + at * D;
+      const uint32_t sdst = smem_u32(scales + st * 2 * Cfg::kScaleBytes) + at * BL;
+      const int64_t soff = static_cast<int64_t>(row) * BL;
+      tma_load_2d(dst, &tmap_k, 0, row, bar);
+      bulk_g2s(sdst, p.k_scales + soff, rows * BL, bar);
+      tma_load_2d(dst + Cfg::kCodeBytes, &tmap_v, 0, row, bar);
+      bulk_g2s(sdst + Cfg::kScaleBytes, p.v_scales + soff, rows * BL, bar);
+    };
+    uint32_t bad = 0;   // bits 2 s, 2 s + 1: the first / second part of the tile in stage s is not there
+    auto issue = [&](int i) {
+      if ((i & 31) == 0) look_up(i);
+      const int st = (turn + i) % kAtStages;
+      const int tok = (tile0 + warp + kAtWarps * i) * kAtTile;
+      const uint32_t bar = smem_u32(&bars[warp * kAtStages + st]);
+      const int pa = __shfl_sync(0xFFFFFFFFu, page_a, i & 31);
+      const bool lost = static_cast<uint32_t>(pa) >= static_cast<uint32_t>(p.pages);
+      uint32_t miss = lost ? 1u : 0u;
+      if (parts == 1) {
+        if (lane == 0) {
+          mbar_arrive_expect_tx(bar, lost ? 0 : kAtTile * 2 * (D + BL));
+          if (!lost) load(st, pa, tok & ((1 << p.page_shift) - 1), kAtTile, 0);
+        }
+      } else {
+        const int pb = __shfl_sync(0xFFFFFFFFu, page_b, i & 31);
+        const bool second = tok + 16 < end, lost_b = second && static_cast<uint32_t>(pb) >= static_cast<uint32_t>(p.pages);
+        miss |= lost_b ? 2u : 0u;
+        if (lane == 0) {
+          mbar_arrive_expect_tx(bar, ((lost ? 0 : 1) + (second && !lost_b ? 1 : 0)) * 16 * 2 * (D + BL));
+          if (!lost) load(st, pa, 0, 16, 0);
+          if (second && !lost_b) load(st, pb, 0, 16, 16);
+        }
+      }
+      if (miss != 0 && lane == 0) atomicOr(&g_device_error, kErrorIndex);
+      bad = (bad & ~(3u << (2 * st))) | (miss << (2 * st));
+    };
+    int issued = 0;
+    for (; issued < kAtStages && issued < n; ++issued) issue(issued);
+
+    // q as the matrix instruction's B fragments, scaled by a power of two per row
+    uint32_t qf[NT][BL][4];
+    float qs[NT][2];      // the factor of rows 2 t4, 2 t4 + 1 on the accumulators
+    int lim[NT][2];       // keys those rows see
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      const int row = row0 + j * 8 + g;
+      float v[BL][8];
+      float amax = 0.0f;
+#pragma unroll
+      for (int b = 0; b < BL; ++b) {
+        uint4 w = make_uint4(0u, 0u, 0u, 0u);
+        if (j * 8 + g < n_rows)
+          w = ld_global_ordered_v4(p.q + (sq.q0 + row / p.group) * p.ldq + static_cast<int64_t>(head * p.group + row % p.group) * D + b * 32 + t4 * 8);
+        unpack_bf16x8(w, v[b]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) amax = fmaxf(amax, fabsf(v[b][i]));
+      }
+      amax = fmaxf(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 1));
+      amax = fmaxf(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 2));
+      const int e = max(static_cast<int>(__float_as_uint(amax) >> 23) - 127, -100);
+      const float up = pow2i(14 - e);
+#pragma unroll
+      for (int b = 0; b < BL; ++b)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const __half2 h = __floats2half2_rn(v[b][2 * i] * up, v[b][2 * i + 1] * up);
+          qf[j][b][i] = *reinterpret_cast<const uint32_t*>(&h);
+        }
+      const float f = p.scale_log2 * pow2i(e - 14);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        qs[j][i] = __shfl_sync(0xFFFFFFFFu, f, (2 * t4 + i) * 4);
+        const int rr = j * 8 + 2 * t4 + i;
+        lim[j][i] = rr < n_rows ? attn_visible(p, sq, (row0 + rr) / p.group) : 0;
+      }
+    }
+    const int full = attn_visible(p, sq, row0 / p.group);   // keys that every row sees
+
+    float o[D / 16][NT][4];
+    float m[NT][2], l[NT][2];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      m[j][0] = m[j][1] = kAtNone;
+      l[j][0] = l[j][1] = 0.0f;
+#pragma unroll
+      for (int c = 0; c < D / 16; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[c][j][i] = 0.0f;
+    }
+
+    const uint32_t mult_addr = smem_u32(mult);
+    for (int i = 0; i < n; ++i) {
+      const int st = (turn + i) % kAtStages;
+      const uint32_t bar = smem_u32(&bars[warp * kAtStages + st]);
+      ok = __all_sync(0xFFFFFFFFu, mbar_wait(bar, ((turn + i) / kAtStages) & 1, &abort_flag));
+      if (!ok) break;
+      const int tok0 = (tile0 + warp + kAtWarps * i) * kAtTile;
+      const uint32_t kt = smem_u32(ring + st * Cfg::kStageBytes), vt = kt + Cfg::kCodeBytes;
+      const uint8_t* ks = scales + st * 2 * Cfg::kScaleBytes;
+      const uint8_t* vs = ks + Cfg::kScaleBytes;
+      const uint32_t miss = (bad >> (2 * st)) & 3u;
+      const bool whole = tok0 + kAtTile <= full && miss == 0;   // every row sees every token
+      const bool here = tok0 + lane < end && !((miss >> (parts == 2 ? lane >> 4 : 0)) & 1u);   // the lane's token
+      if (tok0 + kAtTile > end || miss != 0) {
+        // what stands behind the last token (or on a page that is not there) may be anything, NaN codes too
+        if (!here) {
+#pragma unroll
+          for (int c = 0; c < D / 16; ++c)
+            asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(vt + lane * D + c * 16), "r"(0u) : "memory");
+        }
+      }
+      // the value scales of the lane's token, the tile's common exponent, and the f16 factors 2^(ev - c)
+      int c_tile;
+      {
+        uint32_t w;
+        if (BL == 4) w = *reinterpret_cast<const uint32_t*>(vs + lane * 4);
+        else w = *reinterpret_cast<const uint16_t*>(vs + lane * 2);
+        uint32_t kw;
+        if (BL == 4) kw = *reinterpret_cast<const uint32_t*>(ks + lane * 4);
+        else kw = *reinterpret_cast<const uint16_t*>(ks + lane * 2);
+        uint32_t kf[BL];
+#pragma unroll
+        for (int b = 0; b < BL; ++b) kf[b] = __byte_perm(kw, 0u, 0x0444 | b << 12) >> 1;   // the byte to the exponent field
+        if (BL == 4) *reinterpret_cast<uint4*>(kmult + lane * 4) = make_uint4(kf[0], kf[1], kf[BL - 2], kf[BL - 1]);
+        else *reinterpret_cast<uint2*>(kmult + lane * 2) = make_uint2(kf[0], kf[1]);
+        if (!here) w = 0;
+        uint32_t top = __vmaxu4(w, w >> 16);
+        top = __reduce_max_sync(0xFFFFFFFFu, max(top & 255u, (top >> 8) & 255u));
+        c_tile = max(static_cast<int>(top) - 127 - 7, kAtMinScale);
+        const int at = (lane & 24) | token_frag<D>(lane & 7);
+#pragma unroll
+        for (int b = 0; b < BL; b += 2) {   // two blocks in the halves of a word
+          const uint32_t e = __vmaxs2(__vsub2(__byte_perm(w, 0u, b == 0 ? 0x4140 : 0x4342), (c_tile + 127 - 15) * 0x10001u), 0u);
+          uint32_t f = e << 10;
+          if (__any_sync(0xFFFFFFFFu, (e & 0xFFFFu) == 0u || e < 0x10000u)) {   // a factor below 2^-14: subnormal f16
+            const int d = c_tile + 127;
+            f = f16_pow2(static_cast<int>((w >> (8 * b)) & 255u) - d) | f16_pow2(static_cast<int>((w >> (8 * b + 8)) & 255u) - d) << 16;
+          }
+          mult[b * kAtTile + at] = static_cast<uint16_t>(f);
+          mult[(b + 1) * kAtTile + at] = static_cast<uint16_t>(f >> 16);
+        }
+      }
+      __syncwarp();
+
+      // S^T [32 tokens x rows] in log2 units, plus c
+      float s[2][NT][4];
+#pragma unroll
+      for (int mt = 0; mt < 2; ++mt) {
+        const int ta = mt * 16 + frag_token<D>(g), tb = ta + 8;
+        float fa[BL], fb[BL];
+        if (BL == 4) {
+          *reinterpret_cast<float4*>(fa) = *reinterpret_cast<const float4*>(kmult + ta * 4);
+          *reinterpret_cast<float4*>(fb) = *reinterpret_cast<const float4*>(kmult + tb * 4);
+        } else {
+          *reinterpret_cast<float2*>(fa) = *reinterpret_cast<const float2*>(kmult + ta * 2);
+          *reinterpret_cast<float2*>(fb) = *reinterpret_cast<const float2*>(kmult + tb * 2);
+        }
+#pragma unroll
+        for (int b = 0; b < BL; ++b) {
+          uint32_t a0, a1, b0, b1;
+          asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(a0), "=r"(a1) : "r"(kt + tile_offset<D>(ta, 2 * b + (t4 >> 1)) + (t4 & 1) * 8) : "memory");
+          asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(b0), "=r"(b1) : "r"(kt + tile_offset<D>(tb, 2 * b + (t4 >> 1)) + (t4 & 1) * 8) : "memory");
+          const uint32_t f0[4] = {e4m3x2_to_f16x2(a0), e4m3x2_to_f16x2(b0), e4m3x2_to_f16x2_high(a0), e4m3x2_to_f16x2_high(b0)};
+          const uint32_t f1[4] = {e4m3x2_to_f16x2(a1), e4m3x2_to_f16x2(b1), e4m3x2_to_f16x2_high(a1), e4m3x2_to_f16x2_high(b1)};
+#pragma unroll
+          for (int j = 0; j < NT; ++j) {
+            float d[4];
+            mma_16816_first(d, f0, qf[j][b][0], qf[j][b][1]);
+            mma_16816(d, f1, qf[j][b][2], qf[j][b][3]);
+            s[mt][j][0] = b == 0 ? d[0] * fa[b] : fmaf(d[0], fa[b], s[mt][j][0]);
+            s[mt][j][1] = b == 0 ? d[1] * fa[b] : fmaf(d[1], fa[b], s[mt][j][1]);
+            s[mt][j][2] = b == 0 ? d[2] * fb[b] : fmaf(d[2], fb[b], s[mt][j][2]);
+            s[mt][j][3] = b == 0 ? d[3] * fb[b] : fmaf(d[3], fb[b], s[mt][j][3]);
+          }
+        }
+      }
+      // Weights against the reference m: it follows the maximum only where a score is more than 2^8 above it, so that
+      // most tiles exchange nothing between the lanes and leave the accumulators alone.
+      const float cf = static_cast<float>(c_tile);
+      float z[2][NT][4];
+      auto weigh = [&] {   // exponents of the weights; returns the largest
+        float top = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const float t = cf - m[j][x & 1];
+#pragma unroll
+            for (int mt = 0; mt < 2; ++mt) z[mt][j][x] = fmaf(s[mt][j][x], qs[j][x & 1], t);
+          }
+        if (!whole) {
+#pragma unroll
+          for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+              for (int x = 0; x < 4; ++x) {
+                const int tt = mt * 16 + (x >> 1) * 8 + frag_token<D>(g);
+                if (tok0 + tt >= lim[j][x & 1] || ((miss >> (parts == 2 ? tt >> 4 : 0)) & 1u)) z[mt][j][x] = -INFINITY;
+              }
+        }
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) top = fmaxf(top, fmaxf(z[0][j][x], z[1][j][x]));
+        return top;
+      };
+      if (__any_sync(0xFFFFFFFFu, weigh() > kAtSlack)) {
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            float top = kAtNone;
+#pragma unroll
+            for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+              for (int h = 0; h < 2; ++h)
+                if (z[mt][j][x + 2 * h] > -INFINITY) top = fmaxf(top, fmaf(s[mt][j][x + 2 * h], qs[j][x], cf));
+            top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 4));
+            top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 8));
+            top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 16));
+            const float mn = fmaxf(m[j][x], top), alpha = ex2(m[j][x] - mn);
+            m[j][x] = mn;
+            l[j][x] *= alpha;
+#pragma unroll
+            for (int c = 0; c < D / 16; ++c) {
+              o[c][j][x] *= alpha;
+              o[c][j][x + 2] *= alpha;
+            }
+          }
+        weigh();
+      }
+      uint32_t pf[2][NT][2];
+      const float unscale = pow2i(max(-c_tile, -126));
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          float sum = 0.0f;
+#pragma unroll
+          for (int mt = 0; mt < 2; ++mt) {
+            z[mt][j][x] = ex2(z[mt][j][x]);
+            z[mt][j][x + 2] = ex2(z[mt][j][x + 2]);
+            sum += z[mt][j][x] + z[mt][j][x + 2];
+          }
+          l[j][x] = fmaf(sum, unscale, l[j][x]);
+        }
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const __half2 w = __floats2half2_rn(z[mt][j][2 * h], z[mt][j][2 * h + 1]);
+            pf[mt][j][h] = movmatrix_trans(*reinterpret_cast<const uint32_t*>(&w));
+          }
+      }
+      // O^T += V^T P^T
+#pragma unroll
+      for (int mt = 0; mt < 2; ++mt) {
+        const int row = mt * 16 + ((lane >> 3) & 1) * 8 + frag_token<D>(lane & 7);
+#pragma unroll
+        for (int b = 0; b < BL; ++b) {
+          uint32_t w[4], s0, s1;
+          ldmatrix_x4_trans(w, vt + tile_offset<D>(row, 2 * b + (lane >> 4)));
+          asm volatile("ld.shared.u32 %0, [%1];" : "=r"(s0) : "r"(mult_addr + (b * kAtTile + mt * 16 + 2 * t4) * 2) : "memory");
+          asm volatile("ld.shared.u32 %0, [%1];" : "=r"(s1) : "r"(mult_addr + (b * kAtTile + mt * 16 + 8 + 2 * t4) * 2) : "memory");
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            const uint32_t u0 = __byte_perm(w[2 * c], 0u, 0x3120), u1 = __byte_perm(w[2 * c + 1], 0u, 0x3120);
+            const uint32_t f[4] = {hmul2(e4m3x2_to_f16x2(u0), s0), hmul2(e4m3x2_to_f16x2_high(u0), s0),
+                                   hmul2(e4m3x2_to_f16x2(u1), s1), hmul2(e4m3x2_to_f16x2_high(u1), s1)};
+#pragma unroll
+            for (int j = 0; j < NT; ++j) mma_16816(o[2 * b + c][j], f, pf[mt][j][0], pf[mt][j][1]);
+          }
+        }
+      }
+      __syncwarp();   // every lane is done with the stage
+      if (issued < n) {
+        if (tok0 + kAtTile > end || miss != 0) fence_proxy_async_smem();
+        issue(issued);
+        ++issued;
+      }
+    }
+    turn += n;
+    if (!ok && n > 0) {   // given up: copies already in flight land before the CTA leaves
+      for (int i = max(0, issued - kAtStages); i < issued; ++i) {
+        const uint32_t bar = smem_u32(&bars[warp * kAtStages + (turn - n + i) % kAtStages]);
+        const uint64_t t0 = global_timer_ns();
+        while (!mbar_try_wait(bar, ((turn - n + i) / kAtStages) & 1) && global_timer_ns() - t0 < 100000000ull) {}
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        l[j][x] += __shfl_xor_sync(0xFFFFFFFFu, l[j][x], 4);
+        l[j][x] += __shfl_xor_sync(0xFFFFFFFFu, l[j][x], 8);
+        l[j][x] += __shfl_xor_sync(0xFFFFFFFFu, l[j][x], 16);
+      }
+    // the warps' results meet in the ring: [warp][row][D], then [warp][row] of (m, l)
+    __syncthreads();
+    float* mo = reinterpret_cast<float*>(base);
+    float2* mm = reinterpret_cast<float2*>(mo + kAtWarps * Cfg::kRows * D);
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const int row = j * 8 + 2 * t4 + x;
+        if (g == 0) mm[warp * Cfg::kRows + row] = make_float2(m[j][x] == kAtNone ? -INFINITY : m[j][x], l[j][x]);
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c)
+          *reinterpret_cast<float2*>(mo + (warp * Cfg::kRows + row) * D + c * 16 + 2 * g) = make_float2(o[c][j][x], o[c][j][x + 2]);
+      }
+    }
+    __syncthreads();
+    const bool whole_unit = tile0 == 0 && tile1 == unit_tiles;
+    const int64_t part = static_cast<int64_t>(blockIdx.x) * 2 + (tile0 == 0 ? 1 : 0);
+    if (tile0 == 0 && tile1 < unit_tiles) {   // goes on in the ranges up to the one with its last tile
+      join.parts = (unit0 + unit_tiles - 1) / chunk - static_cast<int>(blockIdx.x) + 1;
+      join.row0 = row0;
+      join.n_rows = n_rows;
+      join.head = head;
+      join.q0 = sq.q0;
+    }
+    for (int i = tid; i < n_rows * (D / 2); i += kAtWarps * 32) {
+      const int row = i / (D / 2), ch = (i % (D / 2)) * 2;
+      float top = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < kAtWarps; ++w) top = fmaxf(top, mm[w * Cfg::kRows + row].x);
+      float sum = 0.0f, a = 0.0f, b = 0.0f;
+#pragma unroll
+      for (int w = 0; w < kAtWarps; ++w) {
+        const float2 ml = mm[w * Cfg::kRows + row];
+        const float f = ml.x == -INFINITY ? 0.0f : ex2(ml.x - top);
+        const float2 v = *reinterpret_cast<const float2*>(mo + (w * Cfg::kRows + row) * D + ch);
+        sum = fmaf(ml.y, f, sum);
+        a = fmaf(v.x, f, a);
+        b = fmaf(v.y, f, b);
+      }
+      if (whole_unit) {
+        const int64_t token = sq.q0 + (row0 + row) / p.group;
+        const int qh = head * p.group + (row0 + row) % p.group;
+        const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+        store_attn_row(p, token, qh, D, ch, a * inv, b * inv);
+        if (ch == 0 && p.lse != nullptr) p.lse[token * p.q_heads + qh] = sum > 0.0f ? (top + log2f(sum)) * 0.69314718055994531f : -INFINITY;
+      } else {
+        *reinterpret_cast<float2*>(p.part_o + (part * Cfg::kRows + row) * D + ch) = make_float2(a, b);
+        if (ch == 0) p.part_ml[part * Cfg::kRows + row] = make_float2(top, sum);
+      }
+    }
+    fence_proxy_async_smem();   // the ring goes back to TMA
+    __syncthreads();
+  }
+  if (tid == 0 && p.join != nullptr) p.join[blockIdx.x] = join;
 }
 
-// Joins the splits of each row, in their order.  One warp per row of a unit.
+// Joins the parts of each unit that more than one range has, in the order of the tokens.  CTA c: the unit that starts in
+// range c; its warps share the rows, and the parts of a row where there are more warps than rows.
 template <int D, int NT>
-__global__ void __launch_bounds__(128) attention_join_kernel(const __grid_constant__ AttnParams p, int64_t n_rows_total) {
+__global__ void __launch_bounds__(NT * 256) attention_join_kernel(const __grid_constant__ AttnParams p) {
   constexpr int kRows = 8 * NT, V = D / 32;
-  const int lane = threadIdx.x & 31;
-  const int64_t r = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 5);
+  constexpr int kBatch = 8 / NT;   // parts whose loads are in flight together; by registers, as all CTAs are to run at once
+  constexpr int kWarps = kRows;
+  __shared__ __align__(16) float sums[kWarps][D];
+  __shared__ float2 mls[kWarps];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  grid_launch_dependents();
   grid_dependency_wait();
-  if (r >= n_rows_total) return;
-  const int row = static_cast<int>(r % kRows);
-  const int64_t unit = r / kRows;
-  const int rt = static_cast<int>(unit % p.row_tiles);
-  const int head = static_cast<int>(unit / p.row_tiles % p.kv_heads);
-  const int seq = static_cast<int>(unit / p.row_tiles / p.kv_heads);
-  const AttnSeq sq = attn_seq(p, seq);
-  const int n_rows = min(kRows, sq.nq * p.group - rt * kRows);
-  if (row >= n_rows) return;
-  const int end = attn_visible(p, sq, (rt * kRows + n_rows - 1) / p.group);
-  const int used = ((end + kAtTile - 1) / kAtTile + p.chunk - 1) / p.chunk;
-  if (used <= 1) return;
-  const int64_t part = unit * p.splits;
-  float top = -INFINITY;
-  for (int s = lane; s < used; s += 32) top = fmaxf(top, p.part_ml[(part + s) * kRows + row].x);
+  const AttnJoin u = p.join[blockIdx.x];
+  if (u.parts <= 0) return;
+  int share = 1;   // warps of a row
+  while (share * 2 * u.n_rows <= kWarps) share *= 2;
+  const int row = warp / share, mine = warp % share;
+  if (row < u.n_rows) {
+    // parts: slot 1 of this range, then slot 0 of the next ones
+    float2 total = make_float2(kAtNone, 0.0f);   // reference, sum
+    float acc[V];
 #pragma unroll
-  for (int x = 16; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, x));
-  const float ref = top == -INFINITY ? 0.0f : top;
-  float sum = 0.0f, acc[V];
+    for (int i = 0; i < V; ++i) acc[i] = 0.0f;
+    for (int i0 = mine; i0 < u.parts; i0 += kBatch * share) {
+      float2 ml[kBatch];
+      float v[kBatch][V];
+      float top = total.x;
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        const int i = i0 + k * share;
+        ml[k] = make_float2(-INFINITY, 0.0f);
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[k][e] = 0.0f;
+        if (i < u.parts) {
+          const int64_t at = ((static_cast<int64_t>(blockIdx.x) + i) * 2 + (i == 0 ? 1 : 0)) * kRows + row;
+          ml[k] = p.part_ml[at];
+          const float* src = p.part_o + at * D + lane * V;
+#pragma unroll
+          for (int e = 0; e < V; e += 2) {
+            const float2 w = *reinterpret_cast<const float2*>(src + e);
+            v[k][e] = w.x;
+            v[k][e + 1] = w.y;
+          }
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) top = fmaxf(top, ml[k].x);
+      const float f0 = ex2(total.x - top);
+      total = make_float2(top, total.y * f0);
+#pragma unroll
+      for (int e = 0; e < V; ++e) acc[e] *= f0;
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        const float f = ex2(ml[k].x - top);   // 0 where the part saw nothing
+        total.y = fmaf(ml[k].y, f, total.y);
+#pragma unroll
+        for (int e = 0; e < V; ++e) acc[e] = fmaf(v[k][e], f, acc[e]);
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < V; e += 2) *reinterpret_cast<float2*>(&sums[warp][lane * V + e]) = make_float2(acc[e], acc[e + 1]);
+    if (lane == 0) mls[warp] = total;
+  }
+  __syncthreads();
+  if (row >= u.n_rows || mine != 0) return;
+  float ref = kAtNone, sum = 0.0f, acc[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) acc[i] = 0.0f;
-#pragma unroll 4
-  for (int s = 0; s < used; ++s) {
-    const float2 ml = p.part_ml[(part + s) * kRows + row];
-    const float f = ex2(ml.x - ref);   // 0 where the split saw nothing
-    const float* src = p.part_o + ((part + s) * kRows + row) * D + lane * V;
-    sum = fmaf(ml.y, f, sum);
+  for (int w = warp; w < warp + share; ++w) ref = fmaxf(ref, mls[w].x);
+  for (int w = warp; w < warp + share; ++w) {
+    const float f = ex2(mls[w].x - ref);
+    sum = fmaf(mls[w].y, f, sum);
 #pragma unroll
-    for (int i = 0; i < V; i += 2) {
-      const float2 v = *reinterpret_cast<const float2*>(src + i);
-      acc[i] = fmaf(v.x, f, acc[i]);
-      acc[i + 1] = fmaf(v.y, f, acc[i + 1]);
-    }
+    for (int e = 0; e < V; ++e) acc[e] = fmaf(sums[w][lane * V + e], f, acc[e]);
   }
-  const int64_t token = sq.q0 + (rt * kRows + row) / p.group;
-  const int qh = head * p.group + (rt * kRows + row) % p.group;
+  const int64_t token = u.q0 + (u.row0 + row) / p.group;
+  const int qh = u.head * p.group + (u.row0 + row) % p.group;
   const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
 #pragma unroll
-  for (int i = 0; i < V; i += 2) store_attn_row(p, token, qh, D, lane * V + i, acc[i] * inv, acc[i + 1] * inv);
+  for (int e = 0; e < V; e += 2) store_attn_row(p, token, qh, D, lane * V + e, acc[e] * inv, acc[e + 1] * inv);
   if (lane == 0 && p.lse != nullptr) p.lse[token * p.q_heads + qh] = sum > 0.0f ? (ref + log2f(sum)) * 0.69314718055994531f : -INFINITY;
 }
 

@@ -1703,49 +1703,48 @@ cudaError_t launch_append(int gc, int grid, const KvAppendParams& p, cudaStream_
   return cudaGetLastError();
 }
 
-// How a call of the attention is cut: rows per CTA, tiles per CTA, CTAs per row tile.
+// How a call of the attention is cut: rows per unit, CTAs, whether a unit may be divided.
 struct AttnPlan {
-  int nt, row_tiles, chunk, splits;
-  int64_t units;   // (sequence, head, row tile)
-  size_t part_o, part_ml, bytes;
+  int nt, grid;
+  bool joins;
+  size_t part_ml, join, bytes;   // offsets in the workspace; the partial sums are its start
 };
-bool plan_attention(const batq_kv_cache* c, int32_t q_heads, int64_t tokens, int32_t seqs, int32_t max_q, int32_t max_kv, AttnPlan* a) {
-  (void)tokens;
+bool plan_attention(const batq_kv_cache* c, int32_t q_heads, int32_t seqs, int32_t max_q, int32_t max_kv, AttnPlan* a) {
   const int64_t rows = static_cast<int64_t>(max_q) * (q_heads / c->kv_heads);
   a->nt = rows <= 8 ? 1 : 2;
-  const int64_t row_tiles = (rows + 8 * a->nt - 1) / (8 * a->nt), units = row_tiles * c->kv_heads * seqs;
-  if (units > (int64_t(1) << 30)) return false;
-  a->row_tiles = static_cast<int>(row_tiles);
-  a->units = units;
+  const int64_t units = (rows + 8 * a->nt - 1) / (8 * a->nt) * c->kv_heads * std::min<int32_t>(seqs, kAtMaxSeqs);
   const int64_t tiles = std::max<int64_t>(1, (static_cast<int64_t>(max_kv) + kAtTile - 1) / kAtTile);
-  const int64_t want = std::max<int64_t>(1, (int64_t(8) * c->sm_count + units - 1) / units);
-  const int64_t chunk = std::max<int64_t>(8, (tiles + want - 1) / want);
-  a->chunk = static_cast<int>(chunk);
-  a->splits = static_cast<int>((tiles + chunk - 1) / chunk);
-  if (units * a->splits > INT_MAX) return false;
-  const size_t parts = a->splits > 1 ? static_cast<size_t>(units) * a->splits * 8 * a->nt : 0;
-  a->part_o = 0;
+  if (units > INT_MAX || units * (tiles + kAtUnitCost) > INT_MAX) return false;   // the kernel counts tiles in 32 bits
+  const int per_sm = c->head_dim == 128 ? (a->nt == 1 ? AttnCfg<128, 1>::kCtasPerSm : AttnCfg<128, 2>::kCtasPerSm)
+                                        : (a->nt == 1 ? AttnCfg<64, 1>::kCtasPerSm : AttnCfg<64, 2>::kCtasPerSm);
+  a->grid = static_cast<int>(std::min<int64_t>(static_cast<int64_t>(per_sm) * c->sm_count, units * tiles));
+  a->joins = tiles > kAtSnap && a->grid > 1;
+  const size_t parts = static_cast<size_t>(a->grid) * 2 * 8 * a->nt;
   a->part_ml = round_up(parts * c->head_dim * sizeof(float), 256);
-  a->bytes = a->part_ml + round_up(parts * sizeof(float2), 256);
+  a->join = a->part_ml + round_up(parts * sizeof(float2), 256);
+  a->bytes = a->joins ? a->join + round_up(a->grid * sizeof(AttnJoin), 256) : 0;
   return true;
 }
 
 template <int D, int NT>
 cudaError_t launch_attention(const batq_kv_cache* c, const AttnPlan& a, const AttnParams& p, cudaStream_t stream) {
-  attention_kv_kernel<D, NT><<<static_cast<unsigned>(a.units * a.splits), kAtWarps * 32, AttnCfg<D, NT>::kSmemBytes, stream>>>(c->tmap_k, c->tmap_v, p);
-  cudaError_t e = cudaGetLastError();
-  if (e != cudaSuccess || a.splits == 1) return e;
-  const int64_t rows = a.units * 8 * NT;
+  // Both wait for the grid in front of them before they touch memory, so that they may be brought onto the SMs while
+  // it still runs.
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(static_cast<unsigned>((rows + 3) / 4));
-  cfg.blockDim = dim3(128);
-  cfg.stream = stream;
   cudaLaunchAttribute attr{};
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, attention_join_kernel<D, NT>, p, rows);
+  cfg.stream = stream;
+  cfg.gridDim = dim3(static_cast<unsigned>(a.grid));
+  cfg.blockDim = dim3(kAtWarps * 32);
+  cfg.dynamicSmemBytes = AttnCfg<D, NT>::kSmemBytes;
+  cudaError_t e = cudaLaunchKernelEx(&cfg, attention_kv_kernel<D, NT>, c->tmap_k, c->tmap_v, p);
+  if (e != cudaSuccess || !a.joins) return e;
+  cfg.blockDim = dim3(NT * 256);
+  cfg.dynamicSmemBytes = 0;
+  return cudaLaunchKernelEx(&cfg, attention_join_kernel<D, NT>, p);
 }
 
 batq_status check_y(const void* y, int32_t y_dtype, int64_t ldy, int64_t m) {
@@ -2706,7 +2705,7 @@ size_t batq_attention_kv_mxfp8_workspace_bytes(const batq_kv_cache* c, int32_t q
   if (c == nullptr || q_heads <= 0 || q_heads % c->kv_heads != 0 || tokens < 0 || seqs < 0 || max_q <= 0 || max_kv < 0) return 0;
   if (tokens == 0 || seqs == 0) return 0;
   AttnPlan a;
-  return plan_attention(c, q_heads, tokens, seqs, max_q, max_kv, &a) ? a.bytes : 0;
+  return plan_attention(c, q_heads, seqs, max_q, max_kv, &a) ? a.bytes : 0;
 }
 
 batq_status batq_attention_kv_mxfp8(const batq_kv_cache* c, const void* q_bf16, int64_t ldq, int32_t q_heads, int64_t tokens,
@@ -2726,7 +2725,7 @@ batq_status batq_attention_kv_mxfp8(const batq_kv_cache* c, const void* q_bf16, 
   if (st != BATQ_OK) return st;
   if (!aligned(q_starts, 4) || !aligned(kv_lens, 4) || !aligned(page_table, 4) || !aligned(lse, 4)) return BATQ_ERR_ALIGN;
   AttnPlan a;
-  if (!plan_attention(c, q_heads, tokens, seqs, max_q, max_kv, &a)) return BATQ_ERR_SHAPE;
+  if (!plan_attention(c, q_heads, seqs, max_q, max_kv, &a)) return BATQ_ERR_SHAPE;
   if (a.bytes > 0) {
     if (workspace == nullptr) return BATQ_ERR_NULL;
     if (!aligned(workspace, 256)) return BATQ_ERR_ALIGN;
@@ -2743,9 +2742,6 @@ batq_status batq_attention_kv_mxfp8(const batq_kv_cache* c, const void* q_bf16, 
   p.kv_heads = c->kv_heads;
   p.group = q_heads / c->kv_heads;
   p.tokens = tokens;
-  p.q_starts = q_starts;
-  p.kv_lens = kv_lens;
-  p.page_table = page_table;
   p.ld_pages = ld_pages;
   p.max_q = max_q;
   p.max_kv = max_kv;
@@ -2758,15 +2754,23 @@ batq_status batq_attention_kv_mxfp8(const batq_kv_cache* c, const void* q_bf16, 
   p.out = static_cast<uint16_t*>(out_bf16);
   p.ldo = ldo;
   p.lse = lse;
-  p.row_tiles = a.row_tiles;
-  p.chunk = a.chunk;
-  p.splits = a.splits;
-  p.part_o = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + a.part_o);
-  p.part_ml = reinterpret_cast<float2*>(static_cast<uint8_t*>(workspace) + a.part_ml);
+  if (a.joins) {
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    p.part_o = reinterpret_cast<float*>(ws);
+    p.part_ml = reinterpret_cast<float2*>(ws + a.part_ml);
+    p.join = reinterpret_cast<AttnJoin*>(ws + a.join);
+  }
   const cudaStream_t cs = static_cast<cudaStream_t>(stream);
-  const cudaError_t e = c->head_dim == 128 ? (a.nt == 1 ? launch_attention<128, 1>(c, a, p, cs) : launch_attention<128, 2>(c, a, p, cs))
-                                           : (a.nt == 1 ? launch_attention<64, 1>(c, a, p, cs) : launch_attention<64, 2>(c, a, p, cs));
-  if (e != cudaSuccess) { cudaGetLastError(); return BATQ_ERR_CUDA; }
+  for (int32_t s0 = 0; s0 < seqs; s0 += kAtMaxSeqs) {   // one after another: they share the workspace
+    p.seqs = std::min<int32_t>(kAtMaxSeqs, seqs - s0);
+    p.seq0 = s0;
+    p.q_starts = q_starts == nullptr ? nullptr : q_starts + s0;
+    p.kv_lens = kv_lens + s0;
+    p.page_table = page_table == nullptr ? nullptr : page_table + static_cast<int64_t>(s0) * ld_pages;
+    const cudaError_t e = c->head_dim == 128 ? (a.nt == 1 ? launch_attention<128, 1>(c, a, p, cs) : launch_attention<128, 2>(c, a, p, cs))
+                                             : (a.nt == 1 ? launch_attention<64, 1>(c, a, p, cs) : launch_attention<64, 2>(c, a, p, cs));
+    if (e != cudaSuccess) { cudaGetLastError(); return BATQ_ERR_CUDA; }
+  }
   return BATQ_OK;
 }
 

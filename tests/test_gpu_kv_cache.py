@@ -131,6 +131,15 @@ def test_prompts(batq, heads, kv_heads, d, page, causal, rows, lens):
     b.check(*b.run(batq, causal=causal), causal=causal)
 
 
+def test_more_sequences_than_one_launch(batq):
+    """1500 short sequences, some empty, some without rows; and without row starts."""
+    lens = [(7 * i) % 70 for i in range(1500)]
+    b = Batch(batq, 4, 2, 64, 16, [(i % 5 != 3) + (i % 11 == 0) for i in range(1500)], lens, seed=18)
+    b.check(*b.run(batq))
+    b = Batch(batq, 4, 2, 64, 16, [1] * 1500, lens, seed=19)
+    b.check(*b.run(batq, use_starts=False))
+
+
 def test_prompt_beside_decoding(batq):
     rows, lens = [1] * 6 + [173] + [1] * 3, [900, 3, 64, 65, 0, 511, 700, 1, 1025, 33]
     b = Batch(batq, 32, 8, 128, 64, rows, lens, seed=5)
