@@ -68,6 +68,7 @@ struct AttnParams {
   int64_t ldo;
   float* lse;                 // [tokens][q_heads] or NULL
   int32_t seqs;               // of this launch, at most kAtMaxSeqs
+  int32_t most_rows;          // sequences with more rows (query rows x group) are another kernel's
   int32_t seq0;               // row of its first sequence where q_starts is NULL
   float* part_o;              // [CTA][2][rows][head_dim]: sums relative to part_ml's reference
   float2* part_ml;            // [CTA][2][rows]: reference exponent m, softmax sum
@@ -190,7 +191,8 @@ __device__ __forceinline__ void store_attn_row(const AttnParams& p, int64_t toke
 __device__ __forceinline__ int attn_tiles(int len) { return max(1, (len + kAtTile - 1) / kAtTile); }
 template <int NT>
 __device__ __forceinline__ int attn_units(const AttnParams& p, const AttnSeq& s) {
-  return p.kv_heads * ((s.nq * p.group + 8 * NT - 1) / (8 * NT));
+  const int rows = s.nq * p.group;
+  return rows > p.most_rows ? 0 : p.kv_heads * ((rows + 8 * NT - 1) / (8 * NT));
 }
 
 template <int D, int NT>

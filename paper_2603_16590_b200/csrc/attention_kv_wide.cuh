@@ -1,0 +1,655 @@
+// Attention over the paged MXFP8 key/value cache for many query rows per key/value head (prompts and chunks of them).
+//
+// The same formulas as attention_kv.cuh; bound by the products, 4 * head_dim * (visible pairs) * q_heads operations, so
+// they run on the 5th-generation tensor cores: tcgen05.mma kind::f16, M = 128 query rows, N = 128 tokens (scores) or
+// head_dim channels (values), fp32 accumulators in tensor memory.  A unit is 256 query rows (two M tiles, rows = query
+// rows x heads of the group, so that a group shares what is read and widened) of one sequence and key/value head.
+//
+//   tensor memory  S0 | S1 | O0 | O1, 128 columns each; the weights P (f16, two per column) overwrite their S and are the
+//                  A operand of the value product from there.
+//   warps 0-7      softmax: a thread owns a row.  While one M tile's warps are in their exponentials, the tensor cores are
+//                  at the other's products.  The reference follows the maximum only beyond 2^8 (as in attention_kv.cuh),
+//                  so O is hardly ever read back before the end.
+//   warps 8-11     widen the codes: K 2^(ek - ck) and V 2^(ev - cv) in f16, ck and cv one integer per 128 tokens, into
+//                  128-byte-swizzled tiles (K: K-major B operand; V: MN-major B operand, the same bytes).  They are widened
+//                  once per 256 rows; the block-scaled kinds would take the codes as they are, but want q and P in 8 bits,
+//                  and V's scales along the wrong axis.
+//   warp 12        TMA: codes and scales, page by page, three tiles ahead
+//   warp 13        issues the MMAs
+//
+// Units go to the CTAs (one per SM) longest first, alternately up and down.  Where there are few, each is divided along
+// its tokens into as many parts as finish soonest; attention_wide_join_kernel adds the parts up in order.
+#pragma once
+#include "attention_kv.cuh"
+#include "gemm_small_s.cuh"
+#include "quantize_act_warp.cuh"
+
+namespace batq {
+
+constexpr int kWdThreads = 512;
+constexpr int kWdRows = 256;        // of a unit
+constexpr int kWdTile = 128;        // tokens
+constexpr int kWdStages = 3;        // of codes, and of f16 tiles
+constexpr int kWdPartCost = 4;      // what a part of a unit costs besides its tiles, in tiles
+
+struct AttnWidePlan { int32_t units, splits; };
+
+struct AttnWideParams {
+  AttnParams a;
+  int32_t least_rows;   // sequences with fewer rows are attention_kv_kernel's
+  int32_t max_items;    // parts of units that the workspace has room for
+  AttnWidePlan* plan;   // written by the first CTA for the join; part_o, part_ml: [item][256 rows], join: [unit]
+};
+
+template <int D>
+struct AttnWideCfg {
+  static constexpr int kBlocks = D / 32;
+  static constexpr int kPanels = D / 64;                         // 64-channel halves of a row: 128 bytes of f16
+  static constexpr int kHalfTile = 128 * 128;                    // 128 rows of one panel
+  static constexpr int kQBytes = 2 * kPanels * kHalfTile;        // two M tiles
+  static constexpr int kF16Bytes = kPanels * kHalfTile;          // one widened tile
+  static constexpr int kCodeBytes = kWdTile * D;
+  static constexpr int kScaleBytes = kWdTile * kBlocks;          // of K or V
+  static constexpr int kScaleSlots = 4;
+  static constexpr int kF16At = kQBytes, kCodeAt = kF16At + kWdStages * kF16Bytes, kScaleAt = kCodeAt + kWdStages * kCodeBytes;
+  static constexpr int kSmemBytes = kScaleAt + kScaleSlots * 2 * kScaleBytes + 1024;
+};
+
+// As f16_idesc_bf16 with f16 operands; b_mn: B is MN-major.
+__host__ __device__ constexpr uint32_t f16_idesc_f16(int M, int N, bool b_mn) {
+  return (1u << 4) | (b_mn ? 1u << 16 : 0u) | (static_cast<uint32_t>(N >> 3) << 17) | (static_cast<uint32_t>(M >> 4) << 24);
+}
+__device__ __forceinline__ void tc_mma_f16(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st_32x32b_x16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
+      ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ uint64_t f32x2_add(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint32_t f16x2_pack(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
+// One part of a unit.
+struct AttnWideItem {
+  AttnSeq sq;
+  int seq, head, row0, n_rows, unit, split;
+  int end;             // keys that the unit's last row sees
+  int tile0, tile1;
+};
+
+template <int D>
+__global__ void __launch_bounds__(kWdThreads, 1)
+attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
+                         const __grid_constant__ AttnWideParams wp) {
+  using Cfg = AttnWideCfg<D>;
+  constexpr int BL = Cfg::kBlocks;
+  const AttnParams& p = wp.a;
+  extern __shared__ __align__(1024) uint8_t wd_smem[];
+  __shared__ __align__(8) uint64_t code_full[kWdStages], code_empty[kWdStages], f16_full[kWdStages], f16_empty[kWdStages];
+  __shared__ __align__(8) uint64_t s_full[2], p_ready[2], o_done[2], q_ready[2], drain;
+  __shared__ int first[kAtMaxSeqs];   // units in front of each sequence's
+  __shared__ int scan_sum[kWdThreads / 32], scan_max[kWdThreads / 32];
+  __shared__ int2 exponents[Cfg::kScaleSlots];   // (ck, cv) of a tile
+  __shared__ uint32_t missing[Cfg::kScaleSlots]; // 16-token pieces of a tile whose page is not there
+  __shared__ uint32_t tmem_base_smem;
+  __shared__ int abort_flag;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(wd_smem) + 1023) & ~uintptr_t(1023));
+
+  grid_launch_dependents();
+  if (tid == 0) {
+    for (int i = 0; i < kWdStages; ++i) {
+      mbar_init(smem_u32(&code_full[i]), 1);
+      mbar_init(smem_u32(&code_empty[i]), 4);
+      mbar_init(smem_u32(&f16_full[i]), 4);
+      mbar_init(smem_u32(&f16_empty[i]), 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(smem_u32(&s_full[i]), 1);
+      mbar_init(smem_u32(&p_ready[i]), 4);
+      mbar_init(smem_u32(&o_done[i]), 1);
+      mbar_init(smem_u32(&q_ready[i]), 4);
+    }
+    mbar_init(smem_u32(&drain), 1);
+    mbar_fence_init();
+    abort_flag = 0;
+    tma_prefetch_desc(&tmap_k);
+    tma_prefetch_desc(&tmap_v);
+  }
+  if (warp == 13) {
+    tmem_alloc(smem_u32(&tmem_base_smem), 512);
+    tmem_relinquish();
+  }
+  grid_dependency_wait();   // q, the lengths and the cache may come from the grid in front
+
+  // units of each sequence, of all, and the most tiles of one
+  int units, splits;
+  {
+    const int s = tid;   // kAtMaxSeqs == kWdThreads
+    int mine = 0, tiles = 0;
+    if (s < p.seqs) {
+      const AttnSeq q = attn_seq(p, s);
+      const int rows = q.nq * p.group;
+      mine = rows >= wp.least_rows ? p.kv_heads * ((rows + kWdRows - 1) / kWdRows) : 0;
+      tiles = mine > 0 ? (q.len + kWdTile - 1) / kWdTile : 0;
+    }
+    int scan = mine;
+#pragma unroll
+    for (int x = 1; x < 32; x <<= 1) {
+      const int v = __shfl_up_sync(0xFFFFFFFFu, scan, x);
+      if (lane >= x) scan += v;
+    }
+    tiles = __reduce_max_sync(0xFFFFFFFFu, tiles);
+    if (lane == 31) scan_sum[warp] = scan;
+    if (lane == 0) scan_max[warp] = tiles;
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    int before = scan - mine;
+    units = tiles = 0;
+    for (int w = 0; w < kWdThreads / 32; ++w) {
+      if (w < warp) before += scan_sum[w];
+      units += scan_sum[w];
+      tiles = max(tiles, scan_max[w]);
+    }
+    first[s] = before;
+    __syncthreads();
+    splits = 1;
+    int best = INT_MAX;
+    const int grid = static_cast<int>(gridDim.x);
+    for (int c = 1; units > 0 && c <= tiles && static_cast<int64_t>(units) * c <= wp.max_items; ++c) {
+      const int cost = (units * c + grid - 1) / grid * ((tiles + c - 1) / c + kWdPartCost);
+      if (cost < best) { best = cost; splits = c; }
+    }
+  }
+  const int items = units * splits;
+  if (tid == 0 && blockIdx.x == 0 && wp.plan != nullptr) *wp.plan = AttnWidePlan{units, splits};
+  const uint32_t tmem = tmem_base_smem;
+
+  // the k-th item of this CTA; false: there is none
+  auto item_at = [&](int k, AttnWideItem* it) {
+    const int grid = static_cast<int>(gridDim.x), b = static_cast<int>(blockIdx.x);
+    const int64_t at = static_cast<int64_t>(k) * grid + ((k & 1) ? grid - 1 - b : b);
+    if (at >= items) return false;
+    const int i = static_cast<int>(at);
+    it->unit = i / splits;
+    it->split = i % splits;
+    int lo = 0, hi = p.seqs - 1;   // the last sequence that starts at or before the unit
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (first[mid] <= it->unit) lo = mid;
+      else hi = mid - 1;
+    }
+    it->seq = lo;
+    it->sq = attn_seq(p, lo);
+    const int rows = it->sq.nq * p.group, row_tiles = (rows + kWdRows - 1) / kWdRows, local = it->unit - first[lo];
+    it->head = local % p.kv_heads;
+    it->row0 = (row_tiles - 1 - local / p.kv_heads) * kWdRows;
+    it->n_rows = min(kWdRows, rows - it->row0);
+    it->end = attn_visible(p, it->sq, (it->row0 + it->n_rows - 1) / p.group);
+    const int64_t tiles = (it->end + kWdTile - 1) / kWdTile;
+    it->tile0 = static_cast<int>(tiles * it->split / splits);
+    it->tile1 = static_cast<int>(tiles * (it->split + 1) / splits);
+    return true;
+  };
+
+  AttnWideItem it;
+  if (warp < 8) {
+    // ------------------------------------------------------------------ softmax: thread = row
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    const int g = warp >> 2, r = tid & 127;
+    const uint32_t lanes = static_cast<uint32_t>(warp & 3) << 21;   // tensor memory lanes of this warp
+    const uint32_t s_at = tmem + lanes + g * 128, o_at = tmem + lanes + 256 + g * 128;
+    uint8_t* qt = base + g * (Cfg::kQBytes / 2) + r * 128;
+    uint32_t s_phase = 0, o_phase = 0;
+    int turn = 0;   // tiles of the CTA in front of this item's: index of exponents, missing
+    bool ok = true;
+    for (int k = 0; ok && item_at(k, &it); ++k) {
+      const int row = it.row0 + g * 128 + r;
+      const bool real = g * 128 + r < it.n_rows, active = g * 128 < it.n_rows;
+      const int qi = row / p.group, qh = it.head * p.group + row % p.group;
+      const int64_t token = it.sq.q0 + qi;
+      const int n = it.tile1 - it.tile0;
+      // q in f16, scaled so that the row's largest element is in [2^14, 2^15); the sign of the scale goes with it
+      float qs = 0.0f;
+      if (active && n > 0) {
+        uint4 w[D / 8];
+        float amax = 0.0f;
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) {
+          w[i] = make_uint4(0u, 0u, 0u, 0u);
+          if (real) w[i] = ld_global_ordered_v4(p.q + token * p.ldq + static_cast<int64_t>(qh) * D + i * 8);
+        }
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) {
+          float v[8];
+          unpack_bf16x8(w[i], v);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(v[e]));
+        }
+        const int e = max(static_cast<int>(__float_as_uint(amax) >> 23) - 127, -100);
+        const float up = p.scale_log2 < 0.0f ? -pow2i(14 - e) : pow2i(14 - e);
+        qs = fmaxf(fabsf(p.scale_log2) * pow2i(e - 14), 1e-37f);
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) {
+          float v[8];
+          unpack_bf16x8(w[i], v);
+          const uint4 h = make_uint4(f16x2_pack(v[0] * up, v[1] * up), f16x2_pack(v[2] * up, v[3] * up),
+                                     f16x2_pack(v[4] * up, v[5] * up), f16x2_pack(v[6] * up, v[7] * up));
+          *reinterpret_cast<uint4*>(qt + (i >> 3) * Cfg::kHalfTile + (((i & 7) ^ (r & 7)) << 4)) = h;
+        }
+        fence_proxy_async_smem();
+        tc_fence_before_sync();   // what was read of tensor memory for the item before
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&q_ready[g]));
+      }
+
+      const int lim = real ? attn_visible(p, it.sq, qi) : 0;            // keys this row sees
+      const int full = attn_visible(p, it.sq, it.row0 / p.group);       // keys that every row sees
+      float m = kAtNone, l = 0.0f;
+      for (int j = 0; active && j < n; ++j) {
+        ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&s_full[g]), s_phase, &abort_flag));
+        if (!ok) break;
+        s_phase ^= 1u;
+        tc_fence_after_sync();
+        const int2 ex = exponents[(turn + j) % Cfg::kScaleSlots];
+        const uint32_t miss = missing[(turn + j) % Cfg::kScaleSlots];
+        uint32_t s[4][32];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) tmem_ld_32x32b_x32(s_at + c * 32, s[c]);
+        tmem_ld_wait();
+        const int tok0 = (it.tile0 + j) * kWdTile;
+        if (tok0 + kWdTile > full || miss != 0) {
+          const int see = lim - tok0;
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (c * 32 + i >= see || ((miss >> (c * 2 + (i >> 4))) & 1u)) s[c][i] = 0xFF800000u;
+        }
+        float top = -INFINITY;
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+          for (int i = 0; i < 32; ++i) top = fmaxf(top, __uint_as_float(s[c][i]));
+        const float qk = fmaxf(qs * pow2i(max(ex.x, -126)), 1e-37f), cv = static_cast<float>(ex.y);
+        if (__any_sync(0xFFFFFFFFu, fmaf(top, qk, cv - m) > kAtSlack)) {
+          const float mn = fmaxf(m, fmaf(top, qk, cv)), alpha = ex2(m - mn);
+          m = mn;
+          l *= alpha;
+          if (j > 0) {   // the value product of the tile before is done: its S was waited for
+#pragma unroll
+            for (int c = 0; c < D / 16; ++c) {
+              uint32_t o[16];
+              tmem_ld_32x32b_x16(o_at + c * 16, o);
+              tmem_ld_wait();
+#pragma unroll
+              for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
+              tmem_st_32x32b_x16(o_at + c * 16, o);
+            }
+          }
+        }
+        const uint64_t qk2 = f32x2_pack(qk, qk), t2 = f32x2_pack(cv - m, cv - m);
+        uint64_t sum0 = 0, sum1 = 0;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          uint32_t w[16];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            float a, b;
+            f32x2_unpack(f32x2_fma(f32x2_pack(__uint_as_float(s[c][2 * i]), __uint_as_float(s[c][2 * i + 1])), qk2, t2), a, b);
+            a = ex2(a);
+            b = ex2(b);
+            if (i & 1) sum1 = f32x2_add(sum1, f32x2_pack(a, b));
+            else sum0 = f32x2_add(sum0, f32x2_pack(a, b));
+            w[i] = f16x2_pack(a, b);
+          }
+          tmem_st_32x32b_x16(s_at + c * 16, w);
+        }
+        float a, b;
+        f32x2_unpack(f32x2_add(sum0, sum1), a, b);
+        l = fmaf(a + b, pow2i(max(-ex.y, -126)), l);
+        tmem_st_wait();
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&p_ready[g]));
+      }
+      if (!ok) break;
+      turn += n;
+      if (!active) continue;
+      if (n > 0) {
+        ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&o_done[g]), o_phase, &abort_flag));
+        if (!ok) break;
+        o_phase ^= 1u;
+        tc_fence_after_sync();
+      }
+      const bool seen = m != kAtNone;
+      const float inv = seen && l > 0.0f ? 1.0f / l : 0.0f;
+      const int64_t part = (static_cast<int64_t>(it.unit) * splits + it.split) * kWdRows + g * 128 + r;
+#pragma unroll
+      for (int c = 0; c < D / 32; ++c) {
+        uint32_t o[32];
+        __syncwarp();
+        if (n > 0) {
+          tmem_ld_32x32b_x32(o_at + c * 32, o);
+          tmem_ld_wait();
+        }
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+          if (n == 0 || !seen) o[i] = 0u;
+        if (real && splits == 1) {
+          uint4* dst = reinterpret_cast<uint4*>(p.out + token * p.ldo + static_cast<int64_t>(qh) * D + c * 32);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            uint32_t w[4];
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {
+              const __nv_bfloat162 v = __floats2bfloat162_rn(__uint_as_float(o[8 * i + 2 * h]) * inv, __uint_as_float(o[8 * i + 2 * h + 1]) * inv);
+              w[h] = *reinterpret_cast<const uint32_t*>(&v);
+            }
+            dst[i] = make_uint4(w[0], w[1], w[2], w[3]);
+          }
+        } else if (real) {
+          uint4* dst = reinterpret_cast<uint4*>(p.part_o + part * D + c * 32);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) dst[i] = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+        }
+      }
+      if (real && splits == 1 && p.lse != nullptr) p.lse[token * p.q_heads + qh] = inv > 0.0f ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
+      if (real && splits > 1) p.part_ml[part] = make_float2(seen ? m : -INFINITY, l);
+      if (splits > 1 && it.split == 0 && tid == 0) p.join[it.unit] = AttnJoin{splits, it.row0, it.n_rows, it.head, it.sq.q0};
+    }
+  } else if (warp < 12) {
+    // ------------------------------------------------------------------ codes -> f16
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    constexpr int kChunks = D / 16, kStep = 128 / kChunks;   // 16-code chunks of a row; rows between a thread's chunks
+    const int ct = tid - 256, c = ct % kChunks, r0 = ct / kChunks, b = c >> 1;
+    uint32_t n_step = 0;   // K and V tiles of the CTA so far: stage n_step % kWdStages
+    int turn = 0;
+    bool ok = true;
+    for (int k = 0; ok && item_at(k, &it); ++k) {
+      for (int t = it.tile0; ok && t < it.tile1; ++t, ++turn) {
+        const int slot = turn % Cfg::kScaleSlots, there = it.end - t * kWdTile;   // tokens of the tile that count
+        const uint8_t* ks = base + Cfg::kScaleAt + slot * 2 * Cfg::kScaleBytes;
+        const uint8_t* vs = ks + Cfg::kScaleBytes;
+        int cs[2] = {0, 0};
+        uint32_t miss = 0;
+#pragma unroll
+        for (int v = 0; v < 2; ++v, ++n_step) {   // K, then V
+          const uint32_t st = n_step % kWdStages, phase = (n_step / kWdStages) & 1u;
+          ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&code_full[st]), phase, &abort_flag) &&
+                                           mbar_wait(smem_u32(&f16_empty[st]), phase ^ 1u, &abort_flag));
+          if (!ok) break;
+          if (v == 0) {   // the tile's exponents, in every warp: a lane has four tokens
+            miss = missing[slot];
+            const bool cut = there < kWdTile || miss != 0;
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+              const uint8_t* src = x == 0 ? ks : vs;
+              uint32_t top = 0;
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                uint32_t w;
+                if (BL == 4) w = *reinterpret_cast<const uint32_t*>(src + (4 * lane + i) * 4);
+                else w = *reinterpret_cast<const uint16_t*>(src + (4 * lane + i) * 2);
+                if (cut && (4 * lane + i >= there || ((miss >> (lane >> 2)) & 1u))) w = 0;
+                top = __vmaxu4(top, w);
+              }
+              top = __vmaxu4(top, top >> 16);
+              top = __reduce_max_sync(0xFFFFFFFFu, max(top & 255u, (top >> 8) & 255u));
+              cs[x] = max(static_cast<int>(top) - 127 - 7, x == 0 ? -100 : kAtMinScale);
+            }
+            if (ct == 0) exponents[slot] = make_int2(cs[0], cs[1]);
+          }
+          const uint8_t* codes = base + Cfg::kCodeAt + st * Cfg::kCodeBytes;
+          uint8_t* dst = base + Cfg::kF16At + st * Cfg::kF16Bytes + (c >> 2) * Cfg::kHalfTile;
+          const uint8_t* sc = v == 0 ? ks : vs;
+#pragma unroll
+          for (int i = 0; i < kChunks; ++i) {
+            const int row = r0 + i * kStep;
+            uint4 w = *reinterpret_cast<const uint4*>(codes + tile_offset<D>(row, c));
+            uint32_t f = f16_pow2(static_cast<int>(sc[row * BL + b]) - 127 - cs[v]) * 0x10001u;
+            if (v == 1 && (row >= there || ((miss >> (row >> 4)) & 1u))) {
+              // behind the last key (or on a page that is not there) anything may stand: values count as zero
+              w = make_uint4(0u, 0u, 0u, 0u);
+              f = 0u;
+            }
+            const uint4 lo = make_uint4(hmul2(e4m3x2_to_f16x2(w.x), f), hmul2(e4m3x2_to_f16x2_high(w.x), f),
+                                        hmul2(e4m3x2_to_f16x2(w.y), f), hmul2(e4m3x2_to_f16x2_high(w.y), f));
+            const uint4 hi = make_uint4(hmul2(e4m3x2_to_f16x2(w.z), f), hmul2(e4m3x2_to_f16x2_high(w.z), f),
+                                        hmul2(e4m3x2_to_f16x2(w.w), f), hmul2(e4m3x2_to_f16x2_high(w.w), f));
+            // the second panel's lanes write their halves in the other order: no two of eight lanes meet in a bank
+            const bool swap = (c & 4) != 0;
+            const int at = (c & 3) * 2;
+            uint8_t* line = dst + row * 128;
+            *reinterpret_cast<uint4*>(line + (((at + (swap ? 1 : 0)) ^ (row & 7)) << 4)) = swap ? hi : lo;
+            *reinterpret_cast<uint4*>(line + (((at + (swap ? 0 : 1)) ^ (row & 7)) << 4)) = swap ? lo : hi;
+          }
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) {
+            mbar_arrive(smem_u32(&code_empty[st]));
+            mbar_arrive(smem_u32(&f16_full[st]));
+          }
+        }
+      }
+    }
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+    if (warp == 12) {
+      // ---------------------------------------------------------------- codes and scales by TMA
+      const int box = min(1 << p.page_shift, 32), boxes = kWdTile / box;   // rows of a copy; copies of a tile
+      uint32_t n_step = 0;
+      int turn = 0;
+      bool ok = true;
+      for (int k = 0; ok && item_at(k, &it); ++k) {
+        const int32_t* pages = p.page_table + static_cast<int64_t>(it.seq) * p.ld_pages;
+        auto look_up = [&](int t) {   // lane = copy
+          const int tok = t * kWdTile + lane * box;
+          return lane < boxes && t < it.tile1 && tok < it.end ? pages[tok >> p.page_shift] : -1;
+        };
+        int next = look_up(it.tile0);
+        for (int t = it.tile0; ok && t < it.tile1; ++t, ++turn) {
+          const int page = next, slot = turn % Cfg::kScaleSlots;
+          next = look_up(t + 1);
+          const int tok = t * kWdTile + lane * box;
+          const bool wanted = lane < boxes && tok < it.end;
+          const bool have = wanted && static_cast<uint32_t>(page) < static_cast<uint32_t>(p.pages);
+          const uint32_t lost = __ballot_sync(0xFFFFFFFFu, wanted && !have);
+          const int n_have = __popc(__ballot_sync(0xFFFFFFFFu, have));
+          const int row = ((page * p.kv_heads + it.head) << p.page_shift) + (tok & ((1 << p.page_shift) - 1));   // below 2^31
+#pragma unroll
+          for (int v = 0; v < 2; ++v, ++n_step) {
+            const uint32_t st = n_step % kWdStages, phase = (n_step / kWdStages) & 1u;
+            ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&code_empty[st]), phase ^ 1u, &abort_flag));
+            if (!ok) break;
+            const uint32_t bar = smem_u32(&code_full[st]);
+            if (lane == 0) {
+              if (v == 0) {
+                uint32_t miss = 0;
+                for (int i = 0; i < boxes; ++i)
+                  if ((lost >> i) & 1u) miss |= (box == 32 ? 3u : 1u) << (i * (box / 16));
+                missing[slot] = miss;
+                if (miss != 0) atomicOr(&g_device_error, kErrorIndex);
+              }
+              mbar_arrive_expect_tx(bar, n_have * box * (D + (v == 0 ? 2 * BL : 0)));
+            }
+            __syncwarp();
+            if (have) {
+              const uint32_t dst = smem_u32(base + Cfg::kCodeAt + st * Cfg::kCodeBytes) + lane * box * D;
+              if (v == 0) {
+                const uint32_t sdst = smem_u32(base + Cfg::kScaleAt + slot * 2 * Cfg::kScaleBytes) + lane * box * BL;
+                tma_load_2d(dst, &tmap_k, 0, row, bar);
+                bulk_g2s(sdst, p.k_scales + static_cast<int64_t>(row) * BL, box * BL, bar);
+                bulk_g2s(sdst + Cfg::kScaleBytes, p.v_scales + static_cast<int64_t>(row) * BL, box * BL, bar);
+              } else {
+                tma_load_2d(dst, &tmap_v, 0, row, bar);
+              }
+            }
+            __syncwarp();
+          }
+        }
+      }
+      if (!ok) {   // given up: copies already in flight land before the CTA leaves
+        for (uint32_t i = n_step > kWdStages ? n_step - kWdStages : 0; i < n_step; ++i) {
+          const uint64_t t0 = global_timer_ns();
+          while (!mbar_try_wait(smem_u32(&code_full[i % kWdStages]), (i / kWdStages) & 1u) && global_timer_ns() - t0 < 100000000ull) {}
+        }
+      }
+    } else if (warp == 13) {
+      // ---------------------------------------------------------------- MMAs
+      constexpr uint32_t idesc_s = f16_idesc_f16(128, kWdTile, false), idesc_o = f16_idesc_f16(128, D, true);
+      const uint64_t q_desc = make_smem_desc(smem_u32(base), 16, 1024, 2);                              // K-major, 128-byte swizzle
+      const uint64_t k_desc = make_smem_desc(smem_u32(base + Cfg::kF16At), 16, 1024, 2);
+      const uint64_t v_desc = make_smem_desc(smem_u32(base + Cfg::kF16At), Cfg::kHalfTile, 1024, 2);    // MN-major: panels, 8 tokens
+      uint32_t n_step = 0, q_phase[2] = {0, 0}, p_phase[2] = {0, 0};
+      bool ok = true;
+      auto wait = [&](uint64_t* bar, uint32_t phase) {
+        ok = ok && __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(bar), phase, &abort_flag));
+        return ok;
+      };
+      auto scores = [&](int g, uint32_t st) {
+        const uint64_t a = q_desc + static_cast<uint32_t>((g * (Cfg::kQBytes / 2)) >> 4);
+        const uint64_t b = k_desc + static_cast<uint32_t>((st * Cfg::kF16Bytes) >> 4);
+        if (elect_one()) {
+#pragma unroll
+          for (int kk = 0; kk < D / 16; ++kk) {
+            const uint32_t off = static_cast<uint32_t>(((kk >> 2) * Cfg::kHalfTile + (kk & 3) * 32) >> 4);
+            tc_mma_f16(tmem + g * 128, a + off, b + off, idesc_s, kk > 0);
+          }
+          tc_commit(smem_u32(&s_full[g]));
+        }
+        __syncwarp();
+      };
+      for (int k = 0; ok && item_at(k, &it); ++k) {
+        const int n = it.tile1 - it.tile0, groups = it.n_rows > 128 ? 2 : 1;
+        if (n <= 0) continue;
+        for (int g = 0; g < groups && wait(&q_ready[g], q_phase[g]); ++g) q_phase[g] ^= 1u;
+        if (!ok) break;
+        // step of tile j: K n_step + 2 j, V n_step + 2 j + 1
+        if (!wait(&f16_full[n_step % kWdStages], (n_step / kWdStages) & 1u)) break;
+        tc_fence_after_sync();
+        for (int g = 0; g < groups; ++g) scores(g, n_step % kWdStages);
+        if (elect_one()) tc_commit(smem_u32(&f16_empty[n_step % kWdStages]));
+        __syncwarp();
+        for (int j = 0; ok && j < n; ++j) {
+          const uint32_t vn = n_step + 2 * j + 1, kn = vn + 1, vst = vn % kWdStages, kst = kn % kWdStages;
+          for (int g = 0; g < groups; ++g) {
+            if (!wait(&p_ready[g], p_phase[g])) break;
+            p_phase[g] ^= 1u;
+            if (g == 0 && !wait(&f16_full[vst], (vn / kWdStages) & 1u)) break;
+            tc_fence_after_sync();
+            if (elect_one()) {
+#pragma unroll
+              for (int kk = 0; kk < kWdTile / 16; ++kk)
+                tc_mma_f16_ta(tmem + 256 + g * 128, tmem + g * 128 + kk * 8, v_desc + static_cast<uint32_t>((vst * Cfg::kF16Bytes + kk * 2048) >> 4),
+                              idesc_o, j > 0 || kk > 0);
+              if (g == groups - 1) tc_commit(smem_u32(&f16_empty[vst]));
+              if (j == n - 1) tc_commit(smem_u32(&o_done[g]));
+            }
+            __syncwarp();
+            if (j + 1 < n) {
+              if (g == 0 && !wait(&f16_full[kst], (kn / kWdStages) & 1u)) break;
+              tc_fence_after_sync();
+              scores(g, kst);
+              if (g == groups - 1) {
+                if (elect_one()) tc_commit(smem_u32(&f16_empty[kst]));
+                __syncwarp();
+              }
+            }
+          }
+        }
+        n_step += 2 * n;
+      }
+      // whatever was issued is over before tensor memory goes back
+      if (elect_one()) tc_commit(smem_u32(&drain));
+      __syncwarp();
+      const uint64_t t0 = global_timer_ns();
+      while (!mbar_try_wait(smem_u32(&drain), 0) && global_timer_ns() - t0 < kWaitLimitNs) {}
+    }
+  }
+  tc_fence_before_sync();
+  __syncthreads();
+  if (warp == 13) {
+    tc_fence_after_sync();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+// Adds the parts of each unit up, in the order of the tokens.  CTA (unit, eight of its rows): one warp per row.
+template <int D>
+__global__ void __launch_bounds__(256) attention_wide_join_kernel(const __grid_constant__ AttnWideParams wp) {
+  constexpr int V = D / 32, kBatch = 4;
+  const AttnParams& p = wp.a;
+  const int lane = threadIdx.x & 31, unit = blockIdx.x, row = blockIdx.y * 8 + (threadIdx.x >> 5);
+  grid_launch_dependents();
+  grid_dependency_wait();
+  const AttnWidePlan plan = *wp.plan;
+  if (plan.splits <= 1 || unit >= plan.units) return;
+  const AttnJoin u = p.join[unit];
+  if (row >= u.n_rows) return;
+  float2 total = make_float2(kAtNone, 0.0f);
+  float acc[V];
+#pragma unroll
+  for (int e = 0; e < V; ++e) acc[e] = 0.0f;
+  for (int i0 = 0; i0 < u.parts; i0 += kBatch) {
+    float2 ml[kBatch];
+    float v[kBatch][V];
+    float top = total.x;
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      ml[k] = make_float2(-INFINITY, 0.0f);
+#pragma unroll
+      for (int e = 0; e < V; ++e) v[k][e] = 0.0f;
+      if (i0 + k < u.parts) {
+        const int64_t at = (static_cast<int64_t>(unit) * plan.splits + i0 + k) * kWdRows + row;
+        ml[k] = p.part_ml[at];
+        const float* src = p.part_o + at * D + lane * V;
+#pragma unroll
+        for (int e = 0; e < V; e += 2) {
+          const float2 w = *reinterpret_cast<const float2*>(src + e);
+          v[k][e] = w.x;
+          v[k][e + 1] = w.y;
+        }
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) top = fmaxf(top, ml[k].x);
+    const float f0 = ex2(total.x - top);
+    total = make_float2(top, total.y * f0);
+#pragma unroll
+    for (int e = 0; e < V; ++e) acc[e] *= f0;
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      const float f = ex2(ml[k].x - top);
+      total.y = fmaf(ml[k].y, f, total.y);
+#pragma unroll
+      for (int e = 0; e < V; ++e) acc[e] = fmaf(v[k][e], f, acc[e]);
+    }
+  }
+  const int64_t token = u.q0 + (u.row0 + row) / p.group;
+  const int qh = u.head * p.group + (u.row0 + row) % p.group;
+  const float inv = total.y > 0.0f ? 1.0f / total.y : 0.0f;
+#pragma unroll
+  for (int e = 0; e < V; e += 2) store_attn_row(p, token, qh, D, lane * V + e, acc[e] * inv, acc[e + 1] * inv);
+  if (lane == 0 && p.lse != nullptr) p.lse[token * p.q_heads + qh] = total.y > 0.0f ? (total.x + log2f(total.y)) * 0.69314718055994531f : -INFINITY;
+}
+
+}  // namespace batq

@@ -16,6 +16,7 @@
 #include <vector>
 
 #include "attention_kv.cuh"
+#include "attention_kv_wide.cuh"
 #include "gemm_mxfp4.cuh"
 #include "gemm_mxfp4_pair.cuh"
 #include "gemm_mxfp4_wide.cuh"
@@ -198,6 +199,8 @@ batq_status device_setup(int* device_out, const DeviceInfo** info_out) {
     e = e ? e : set_smem(attention_kv_kernel<128, 2>, AttnCfg<128, 2>::kSmemBytes);
     e = e ? e : set_smem(attention_kv_kernel<64, 1>, AttnCfg<64, 1>::kSmemBytes);
     e = e ? e : set_smem(attention_kv_kernel<64, 2>, AttnCfg<64, 2>::kSmemBytes);
+    e = e ? e : set_smem(attention_kv_wide_kernel<128>, AttnWideCfg<128>::kSmemBytes);
+    e = e ? e : set_smem(attention_kv_wide_kernel<64>, AttnWideCfg<64>::kSmemBytes);
     if (e != cudaSuccess) { cudaGetLastError(); return BATQ_ERR_CUDA; }
     if (g_encode_tiled == nullptr) {
       void* fn = nullptr;
@@ -1703,33 +1706,61 @@ cudaError_t launch_append(int gc, int grid, const KvAppendParams& p, cudaStream_
   return cudaGetLastError();
 }
 
-// How a call of the attention is cut: rows per unit, CTAs, whether a unit may be divided.
+// How a call of the attention is cut.  Sequences with up to kNarrowRows rows (query rows x heads of the group) go to
+// attention_kv_kernel, the others to attention_kv_wide_kernel; a call of one sequence that may have more makes one
+// launch only.
+constexpr int kNarrowRows = 32;
 struct AttnPlan {
-  int nt, grid;
-  bool joins;
-  size_t part_ml, join, bytes;   // offsets in the workspace; the partial sums are its start
+  bool narrow, wide;
+  int nt, grid;                         // narrow: rows of a unit / 8, CTAs
+  bool joins;                           //         whether a unit may be divided
+  int wide_grid, wide_items, wide_units;
+  size_t part_ml, join;                 // offsets of the narrow part's workspace; the partial sums are its start
+  size_t wide_o, wide_ml, wide_join, wide_plan;
+  size_t bytes;
 };
 bool plan_attention(const batq_kv_cache* c, int32_t q_heads, int32_t seqs, int32_t max_q, int32_t max_kv, AttnPlan* a) {
-  const int64_t rows = static_cast<int64_t>(max_q) * (q_heads / c->kv_heads);
-  a->nt = rows <= 8 ? 1 : 2;
-  const int64_t units = (rows + 8 * a->nt - 1) / (8 * a->nt) * c->kv_heads * std::min<int32_t>(seqs, kAtMaxSeqs);
-  const int64_t tiles = std::max<int64_t>(1, (static_cast<int64_t>(max_kv) + kAtTile - 1) / kAtTile);
-  if (units > INT_MAX || units * (tiles + kAtUnitCost) > INT_MAX) return false;   // the kernel counts tiles in 32 bits
-  const int per_sm = c->head_dim == 128 ? (a->nt == 1 ? AttnCfg<128, 1>::kCtasPerSm : AttnCfg<128, 2>::kCtasPerSm)
-                                        : (a->nt == 1 ? AttnCfg<64, 1>::kCtasPerSm : AttnCfg<64, 2>::kCtasPerSm);
-  a->grid = static_cast<int>(std::min<int64_t>(static_cast<int64_t>(per_sm) * c->sm_count, units * tiles));
-  a->joins = tiles > kAtSnap && a->grid > 1;
-  const size_t parts = static_cast<size_t>(a->grid) * 2 * 8 * a->nt;
-  a->part_ml = round_up(parts * c->head_dim * sizeof(float), 256);
-  a->join = a->part_ml + round_up(parts * sizeof(float2), 256);
-  a->bytes = a->joins ? a->join + round_up(a->grid * sizeof(AttnJoin), 256) : 0;
+  *a = AttnPlan{};
+  const int64_t group = q_heads / c->kv_heads, most = max_q * group, batch = std::min<int32_t>(seqs, kAtMaxSeqs);
+  a->wide = most > kNarrowRows;
+  a->narrow = !a->wide || seqs > 1;
+  if (a->narrow) {
+    const int64_t rows = std::min<int64_t>(most, kNarrowRows);
+    a->nt = rows <= 8 ? 1 : 2;
+    const int64_t units = (rows + 8 * a->nt - 1) / (8 * a->nt) * c->kv_heads * batch;
+    const int64_t tiles = std::max<int64_t>(1, (static_cast<int64_t>(max_kv) + kAtTile - 1) / kAtTile);
+    if (units > INT_MAX || units * (tiles + kAtUnitCost) > INT_MAX) return false;   // the kernel counts tiles in 32 bits
+    const int per_sm = c->head_dim == 128 ? (a->nt == 1 ? AttnCfg<128, 1>::kCtasPerSm : AttnCfg<128, 2>::kCtasPerSm)
+                                          : (a->nt == 1 ? AttnCfg<64, 1>::kCtasPerSm : AttnCfg<64, 2>::kCtasPerSm);
+    a->grid = static_cast<int>(std::min<int64_t>(static_cast<int64_t>(per_sm) * c->sm_count, units * tiles));
+    a->joins = tiles > kAtSnap && a->grid > 1;
+    const size_t parts = static_cast<size_t>(a->grid) * 2 * 8 * a->nt;
+    a->part_ml = round_up(parts * c->head_dim * sizeof(float), 256);
+    a->join = a->part_ml + round_up(parts * sizeof(float2), 256);
+    a->bytes = a->joins ? a->join + round_up(a->grid * sizeof(AttnJoin), 256) : 0;
+  }
+  if (a->wide) {
+    const int64_t units = (most + kWdRows - 1) / kWdRows * c->kv_heads * batch;
+    const int64_t tiles = (static_cast<int64_t>(max_kv) + kWdTile - 1) / kWdTile;
+    if (most > INT_MAX / 2 || units > INT_MAX / 1024 || tiles * 1024 > INT_MAX) return false;
+    // parts: two for each SM at most, and none where the units alone may be as many
+    a->wide_items = static_cast<int>(std::min<int64_t>(2 * c->sm_count, units * std::max<int64_t>(1, tiles)));
+    a->wide_units = static_cast<int>(std::min<int64_t>(units, a->wide_items / 2));
+    a->wide_grid = static_cast<int>(std::min<int64_t>(c->sm_count, units * std::max<int64_t>(1, tiles)));
+    const size_t rows = static_cast<size_t>(a->wide_items) * kWdRows;
+    a->wide_o = a->bytes;
+    a->wide_ml = a->wide_o + round_up(rows * c->head_dim * sizeof(float), 256);
+    a->wide_join = a->wide_ml + round_up(rows * sizeof(float2), 256);
+    a->wide_plan = a->wide_join + round_up((a->wide_units + 1) * sizeof(AttnJoin), 256);
+    a->bytes = a->wide_plan + 256;
+  }
   return true;
 }
 
-template <int D, int NT>
-cudaError_t launch_attention(const batq_kv_cache* c, const AttnPlan& a, const AttnParams& p, cudaStream_t stream) {
-  // Both wait for the grid in front of them before they touch memory, so that they may be brought onto the SMs while
-  // it still runs.
+// Every kernel of the attention waits for the grid in front of it before it touches memory, so that it may be brought
+// onto the SMs while that one still runs.
+template <typename... Formal, typename... Actual>
+cudaError_t launch_dependent(void (*kernel)(Formal...), dim3 grid, int threads, size_t smem, cudaStream_t stream, const Actual&... args) {
   cudaLaunchConfig_t cfg{};
   cudaLaunchAttribute attr{};
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -1737,14 +1768,25 @@ cudaError_t launch_attention(const batq_kv_cache* c, const AttnPlan& a, const At
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
   cfg.stream = stream;
-  cfg.gridDim = dim3(static_cast<unsigned>(a.grid));
-  cfg.blockDim = dim3(kAtWarps * 32);
-  cfg.dynamicSmemBytes = AttnCfg<D, NT>::kSmemBytes;
-  cudaError_t e = cudaLaunchKernelEx(&cfg, attention_kv_kernel<D, NT>, c->tmap_k, c->tmap_v, p);
-  if (e != cudaSuccess || !a.joins) return e;
-  cfg.blockDim = dim3(NT * 256);
-  cfg.dynamicSmemBytes = 0;
-  return cudaLaunchKernelEx(&cfg, attention_join_kernel<D, NT>, p);
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(static_cast<unsigned>(threads));
+  cfg.dynamicSmemBytes = smem;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+template <int D, int NT>
+cudaError_t launch_attention(const batq_kv_cache* c, const AttnPlan& a, const AttnParams& p, cudaStream_t stream) {
+  const dim3 grid(static_cast<unsigned>(a.grid));
+  const cudaError_t e = launch_dependent(attention_kv_kernel<D, NT>, grid, kAtWarps * 32, AttnCfg<D, NT>::kSmemBytes, stream, c->tmap_k, c->tmap_v, p);
+  return e != cudaSuccess || !a.joins ? e : launch_dependent(attention_join_kernel<D, NT>, grid, NT * 256, 0, stream, p);
+}
+
+template <int D>
+cudaError_t launch_attention_wide(const batq_kv_cache* c, const AttnPlan& a, const AttnWideParams& p, cudaStream_t stream) {
+  const cudaError_t e = launch_dependent(attention_kv_wide_kernel<D>, dim3(static_cast<unsigned>(a.wide_grid)), kWdThreads, AttnWideCfg<D>::kSmemBytes,
+                                         stream, c->tmap_k, c->tmap_v, p);
+  if (e != cudaSuccess || a.wide_units == 0) return e;
+  return launch_dependent(attention_wide_join_kernel<D>, dim3(static_cast<unsigned>(a.wide_units), kWdRows / 8), 256, 0, stream, p);
 }
 
 batq_status check_y(const void* y, int32_t y_dtype, int64_t ldy, int64_t m) {
@@ -2754,12 +2796,8 @@ batq_status batq_attention_kv_mxfp8(const batq_kv_cache* c, const void* q_bf16, 
   p.out = static_cast<uint16_t*>(out_bf16);
   p.ldo = ldo;
   p.lse = lse;
-  if (a.joins) {
-    uint8_t* ws = static_cast<uint8_t*>(workspace);
-    p.part_o = reinterpret_cast<float*>(ws);
-    p.part_ml = reinterpret_cast<float2*>(ws + a.part_ml);
-    p.join = reinterpret_cast<AttnJoin*>(ws + a.join);
-  }
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  AttnWideParams wp{};
   const cudaStream_t cs = static_cast<cudaStream_t>(stream);
   for (int32_t s0 = 0; s0 < seqs; s0 += kAtMaxSeqs) {   // one after another: they share the workspace
     p.seqs = std::min<int32_t>(kAtMaxSeqs, seqs - s0);
@@ -2767,8 +2805,25 @@ batq_status batq_attention_kv_mxfp8(const batq_kv_cache* c, const void* q_bf16, 
     p.q_starts = q_starts == nullptr ? nullptr : q_starts + s0;
     p.kv_lens = kv_lens + s0;
     p.page_table = page_table == nullptr ? nullptr : page_table + static_cast<int64_t>(s0) * ld_pages;
-    const cudaError_t e = c->head_dim == 128 ? (a.nt == 1 ? launch_attention<128, 1>(c, a, p, cs) : launch_attention<128, 2>(c, a, p, cs))
-                                             : (a.nt == 1 ? launch_attention<64, 1>(c, a, p, cs) : launch_attention<64, 2>(c, a, p, cs));
+    cudaError_t e = cudaSuccess;
+    if (a.narrow) {
+      p.most_rows = a.wide ? kNarrowRows : INT_MAX;
+      p.part_o = a.joins ? reinterpret_cast<float*>(ws) : nullptr;
+      p.part_ml = a.joins ? reinterpret_cast<float2*>(ws + a.part_ml) : nullptr;
+      p.join = a.joins ? reinterpret_cast<AttnJoin*>(ws + a.join) : nullptr;
+      e = c->head_dim == 128 ? (a.nt == 1 ? launch_attention<128, 1>(c, a, p, cs) : launch_attention<128, 2>(c, a, p, cs))
+                             : (a.nt == 1 ? launch_attention<64, 1>(c, a, p, cs) : launch_attention<64, 2>(c, a, p, cs));
+    }
+    if (e == cudaSuccess && a.wide) {
+      wp.a = p;
+      wp.a.part_o = reinterpret_cast<float*>(ws + a.wide_o);
+      wp.a.part_ml = reinterpret_cast<float2*>(ws + a.wide_ml);
+      wp.a.join = reinterpret_cast<AttnJoin*>(ws + a.wide_join);
+      wp.plan = reinterpret_cast<AttnWidePlan*>(ws + a.wide_plan);
+      wp.least_rows = a.narrow ? kNarrowRows + 1 : 1;
+      wp.max_items = a.wide_items;
+      e = c->head_dim == 128 ? launch_attention_wide<128>(c, a, wp, cs) : launch_attention_wide<64>(c, a, wp, cs);
+    }
     if (e != cudaSuccess) { cudaGetLastError(); return BATQ_ERR_CUDA; }
   }
   return BATQ_OK;
