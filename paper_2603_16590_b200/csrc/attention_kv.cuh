@@ -152,9 +152,9 @@ __device__ __forceinline__ uint32_t movmatrix_trans(uint32_t a) {
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(a));
   return r;
 }
-__device__ __forceinline__ float ex2(float x) {
+__device__ __forceinline__ float ex2(float x) {   // results below 2^-126 are 0: nothing here tells them from it
   float r;
-  asm("ex2.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
 __device__ __forceinline__ float pow2i(int e) {   // 2^e, e in [-126, 127]
@@ -163,6 +163,13 @@ __device__ __forceinline__ float pow2i(int e) {   // 2^e, e in [-126, 127]
 // 2^e as f16 bits; 0 below 2^-24 (e <= 7 here).
 __device__ __forceinline__ uint32_t f16_pow2(int e) {
   return e >= -14 ? static_cast<uint32_t>(e + 15) << 10 : e >= -24 ? 1u << (e + 24) : 0u;
+}
+// The same of two scale bytes in the halves of a word, less d (the whole warp calls it).
+__device__ __forceinline__ uint32_t f16_pow2x2(uint32_t bytes, int d) {
+  const uint32_t e = __vmaxs2(__vsub2(bytes, (d - 15) * 0x10001u), 0u);
+  if (__any_sync(0xFFFFFFFFu, (e & 0xFFFFu) == 0u || e < 0x10000u))   // a factor below 2^-14: subnormal f16
+    return f16_pow2(static_cast<int>(bytes & 0xFFFFu) - d) | f16_pow2(static_cast<int>(bytes >> 16) - d) << 16;
+  return e << 10;
 }
 
 // The token of a tile's eight-token group that stands in row i of a matrix fragment.  Rows 0..3 are read by the first
@@ -421,7 +428,7 @@ attention_kv_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
     for (int i = 0; i < n; ++i) {
       const int st = (turn + i) % kAtStages;
       const uint32_t bar = smem_u32(&bars[warp * kAtStages + st]);
-      ok = __all_sync(0xFFFFFFFFu, mbar_wait(bar, ((turn + i) / kAtStages) & 1, &abort_flag));
+      ok = __all_sync(0xFFFFFFFFu, mbar_wait_short(bar, ((turn + i) / kAtStages) & 1, &abort_flag));
       if (!ok) break;
       const int tok0 = (tile0 + warp + kAtWarps * i) * kAtTile;
       const uint32_t kt = smem_u32(ring + st * Cfg::kStageBytes), vt = kt + Cfg::kCodeBytes;
@@ -459,12 +466,7 @@ attention_kv_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
         const int at = (lane & 24) | token_frag<D>(lane & 7);
 #pragma unroll
         for (int b = 0; b < BL; b += 2) {   // two blocks in the halves of a word
-          const uint32_t e = __vmaxs2(__vsub2(__byte_perm(w, 0u, b == 0 ? 0x4140 : 0x4342), (c_tile + 127 - 15) * 0x10001u), 0u);
-          uint32_t f = e << 10;
-          if (__any_sync(0xFFFFFFFFu, (e & 0xFFFFu) == 0u || e < 0x10000u)) {   // a factor below 2^-14: subnormal f16
-            const int d = c_tile + 127;
-            f = f16_pow2(static_cast<int>((w >> (8 * b)) & 255u) - d) | f16_pow2(static_cast<int>((w >> (8 * b + 8)) & 255u) - d) << 16;
-          }
+          const uint32_t f = f16_pow2x2(__byte_perm(w, 0u, b == 0 ? 0x4140 : 0x4342), c_tile + 127);
           mult[b * kAtTile + at] = static_cast<uint16_t>(f);
           mult[(b + 1) * kAtTile + at] = static_cast<uint16_t>(f >> 16);
         }

@@ -20,6 +20,8 @@
 // Units go to the CTAs (one per SM) longest first, alternately up and down.  Where there are few, each is divided along
 // its tokens into as many parts as finish soonest; attention_wide_join_kernel adds the parts up in order.
 #pragma once
+#include <type_traits>
+
 #include "attention_kv.cuh"
 #include "gemm_small_s.cuh"
 #include "quantize_act_warp.cuh"
@@ -30,6 +32,9 @@ constexpr int kWdThreads = 512;
 constexpr int kWdRows = 256;        // of a unit
 constexpr int kWdTile = 128;        // tokens
 constexpr int kWdStages = 3;        // of codes, and of f16 tiles
+// Registers of a thread of the softmax warps (which hold 128 scores), the widening ones and the others.
+constexpr int kWdRegsSoftmax = 192, kWdRegsWiden = 80, kWdRegsIssue = 48;
+static_assert(256 * kWdRegsSoftmax + 128 * kWdRegsWiden + 128 * kWdRegsIssue <= 65536, "what the block is launched with: 128 each");
 constexpr int kWdPartCost = 4;      // what a part of a unit costs besides its tiles, in tiles
 
 struct AttnWidePlan { int32_t units, splits; };
@@ -74,6 +79,23 @@ __device__ __forceinline__ void tmem_st_32x32b_x16(uint32_t taddr, const uint32_
       "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr)
       : "memory");
 }
+// Waits for the loads in front; the registers that one of them fills are named so that nothing that uses them can be
+// moved ahead of the wait.
+__device__ __forceinline__ void tmem_ld_wait_for(uint32_t (&r)[32]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]),
+                 "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]),
+                 "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
+               :
+               : "memory");
+}
+__device__ __forceinline__ void tmem_ld_wait_for(uint32_t (&r)[16]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]),
+                 "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
+               :
+               : "memory");
+}
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ uint64_t f32x2_add(uint64_t a, uint64_t b) {
   uint64_t r;
@@ -85,6 +107,12 @@ __device__ __forceinline__ uint32_t f16x2_pack(float lo, float hi) {
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
 }
+
+// 16 bytes global -> shared, the rest behind `bytes` as zeros; waiting for all of the thread's.
+__device__ __forceinline__ void cp_async_16(uint32_t dst_smem, const void* src, int bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst_smem), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void cp_async_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
 // One part of a unit.
 struct AttnWideItem {
@@ -108,6 +136,8 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
   __shared__ int scan_sum[kWdThreads / 32], scan_max[kWdThreads / 32];
   __shared__ int2 exponents[Cfg::kScaleSlots];   // (ck, cv) of a tile
   __shared__ uint32_t missing[Cfg::kScaleSlots]; // 16-token pieces of a tile whose page is not there
+  // 2^(e - c) of a tile's keys, values: f16, [block][token % 8][token / 8], so that a widening thread's are one run
+  __shared__ __align__(16) uint16_t factors[2][kWdTile * BL];
   __shared__ uint32_t tmem_base_smem;
   __shared__ int abort_flag;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -181,7 +211,7 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
   }
   const int items = units * splits;
   if (tid == 0 && blockIdx.x == 0 && wp.plan != nullptr) *wp.plan = AttnWidePlan{units, splits};
-  const uint32_t tmem = tmem_base_smem;
+  const uint32_t tmem = 0;   // all 512 columns are this CTA's
 
   // the k-th item of this CTA; false: there is none
   auto item_at = [&](int k, AttnWideItem* it) {
@@ -213,7 +243,7 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
   AttnWideItem it;
   if (warp < 8) {
     // ------------------------------------------------------------------ softmax: thread = row
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kWdRegsSoftmax));
     const int g = warp >> 2, r = tid & 127;
     const uint32_t lanes = static_cast<uint32_t>(warp & 3) << 21;   // tensor memory lanes of this warp
     const uint32_t s_at = tmem + lanes + g * 128, o_at = tmem + lanes + 256 + g * 128;
@@ -230,17 +260,24 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
       // q in f16, scaled so that the row's largest element is in [2^14, 2^15); the sign of the scale goes with it
       float qs = 0.0f;
       if (active && n > 0) {
-        uint4 w[D / 8];
+        // The warp brings its 32 rows as they are, whole rows at a time, to where they will stand in f16; then each
+        // thread turns its own.
+        const int64_t q_off = token * p.ldq + static_cast<int64_t>(qh) * D;
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) {
+          const int at = i * (256 / D) + lane / (D / 8), ch = lane % (D / 8), rr = (warp & 3) * 32 + at;
+          const int64_t off = __shfl_sync(0xFFFFFFFFu, q_off, at);
+          const bool there = __shfl_sync(0xFFFFFFFFu, real, at);
+          cp_async_16(smem_u32(base + g * (Cfg::kQBytes / 2) + rr * 128 + (ch >> 3) * Cfg::kHalfTile + (((ch & 7) ^ (rr & 7)) << 4)),
+                      p.q + (there ? off : 0) + ch * 8, there ? 16 : 0);
+        }
+        cp_async_wait_all();
+        __syncwarp();
         float amax = 0.0f;
 #pragma unroll
         for (int i = 0; i < D / 8; ++i) {
-          w[i] = make_uint4(0u, 0u, 0u, 0u);
-          if (real) w[i] = ld_global_ordered_v4(p.q + token * p.ldq + static_cast<int64_t>(qh) * D + i * 8);
-        }
-#pragma unroll
-        for (int i = 0; i < D / 8; ++i) {
           float v[8];
-          unpack_bf16x8(w[i], v);
+          unpack_bf16x8(*reinterpret_cast<const uint4*>(qt + (i >> 3) * Cfg::kHalfTile + (((i & 7) ^ (r & 7)) << 4)), v);
 #pragma unroll
           for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(v[e]));
         }
@@ -249,11 +286,11 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
         qs = fmaxf(fabsf(p.scale_log2) * pow2i(e - 14), 1e-37f);
 #pragma unroll
         for (int i = 0; i < D / 8; ++i) {
+          uint4* at = reinterpret_cast<uint4*>(qt + (i >> 3) * Cfg::kHalfTile + (((i & 7) ^ (r & 7)) << 4));
           float v[8];
-          unpack_bf16x8(w[i], v);
-          const uint4 h = make_uint4(f16x2_pack(v[0] * up, v[1] * up), f16x2_pack(v[2] * up, v[3] * up),
-                                     f16x2_pack(v[4] * up, v[5] * up), f16x2_pack(v[6] * up, v[7] * up));
-          *reinterpret_cast<uint4*>(qt + (i >> 3) * Cfg::kHalfTile + (((i & 7) ^ (r & 7)) << 4)) = h;
+          unpack_bf16x8(*at, v);
+          *at = make_uint4(f16x2_pack(v[0] * up, v[1] * up), f16x2_pack(v[2] * up, v[3] * up), f16x2_pack(v[4] * up, v[5] * up),
+                           f16x2_pack(v[6] * up, v[7] * up));
         }
         fence_proxy_async_smem();
         tc_fence_before_sync();   // what was read of tensor memory for the item before
@@ -265,30 +302,41 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
       const int full = attn_visible(p, it.sq, it.row0 / p.group);       // keys that every row sees
       float m = kAtNone, l = 0.0f;
       for (int j = 0; active && j < n; ++j) {
-        ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&s_full[g]), s_phase, &abort_flag));
+        ok = __all_sync(0xFFFFFFFFu, mbar_wait_short(smem_u32(&s_full[g]), s_phase, &abort_flag));
         if (!ok) break;
         s_phase ^= 1u;
         tc_fence_after_sync();
         const int2 ex = exponents[(turn + j) % Cfg::kScaleSlots];
         const uint32_t miss = missing[(turn + j) % Cfg::kScaleSlots];
+        const int tok0 = (it.tile0 + j) * kWdTile, see = lim - tok0;
+        const bool part = tok0 + kWdTile > full || miss != 0;
         uint32_t s[4][32];
 #pragma unroll
         for (int c = 0; c < 4; ++c) tmem_ld_32x32b_x32(s_at + c * 32, s[c]);
-        tmem_ld_wait();
-        const int tok0 = (it.tile0 + j) * kWdTile;
-        if (tok0 + kWdTile > full || miss != 0) {
-          const int see = lim - tok0;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) tmem_ld_wait_for(s[c]);
+        if (part) {
 #pragma unroll
           for (int c = 0; c < 4; ++c)
 #pragma unroll
             for (int i = 0; i < 32; ++i)
-              if (c * 32 + i >= see || ((miss >> (c * 2 + (i >> 4))) & 1u)) s[c][i] = 0xFF800000u;
+              if (c * 32 + i >= see) s[c][i] = 0xFF800000u;
+          if (miss != 0) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+              for (int i = 0; i < 32; ++i)
+                if ((miss >> (c * 2 + (i >> 4))) & 1u) s[c][i] = 0xFF800000u;
+          }
         }
-        float top = -INFINITY;
+        float tops[4];   // four chains: one takes 10 cycles a step
 #pragma unroll
-        for (int c = 0; c < 4; ++c)
+        for (int c = 0; c < 4; ++c) {
+          tops[c] = __uint_as_float(s[c][0]);
 #pragma unroll
-          for (int i = 0; i < 32; ++i) top = fmaxf(top, __uint_as_float(s[c][i]));
+          for (int i = 1; i < 32; ++i) tops[c] = fmaxf(tops[c], __uint_as_float(s[c][i]));
+        }
+        const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
         const float qk = fmaxf(qs * pow2i(max(ex.x, -126)), 1e-37f), cv = static_cast<float>(ex.y);
         if (__any_sync(0xFFFFFFFFu, fmaf(top, qk, cv - m) > kAtSlack)) {
           const float mn = fmaxf(m, fmaf(top, qk, cv)), alpha = ex2(m - mn);
@@ -299,7 +347,7 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
             for (int c = 0; c < D / 16; ++c) {
               uint32_t o[16];
               tmem_ld_32x32b_x16(o_at + c * 16, o);
-              tmem_ld_wait();
+              tmem_ld_wait_for(o);
 #pragma unroll
               for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
               tmem_st_32x32b_x16(o_at + c * 16, o);
@@ -310,11 +358,12 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
         uint64_t sum0 = 0, sum1 = 0;
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
+          const uint32_t (&x)[32] = s[c];
           uint32_t w[16];
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             float a, b;
-            f32x2_unpack(f32x2_fma(f32x2_pack(__uint_as_float(s[c][2 * i]), __uint_as_float(s[c][2 * i + 1])), qk2, t2), a, b);
+            f32x2_unpack(f32x2_fma(f32x2_pack(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), qk2, t2), a, b);
             a = ex2(a);
             b = ex2(b);
             if (i & 1) sum1 = f32x2_add(sum1, f32x2_pack(a, b));
@@ -335,7 +384,7 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
       turn += n;
       if (!active) continue;
       if (n > 0) {
-        ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&o_done[g]), o_phase, &abort_flag));
+        ok = __all_sync(0xFFFFFFFFu, mbar_wait_short(smem_u32(&o_done[g]), o_phase, &abort_flag));
         if (!ok) break;
         o_phase ^= 1u;
         tc_fence_after_sync();
@@ -349,13 +398,12 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
         __syncwarp();
         if (n > 0) {
           tmem_ld_32x32b_x32(o_at + c * 32, o);
-          tmem_ld_wait();
+          tmem_ld_wait_for(o);
         }
 #pragma unroll
         for (int i = 0; i < 32; ++i)
           if (n == 0 || !seen) o[i] = 0u;
-        if (real && splits == 1) {
-          uint4* dst = reinterpret_cast<uint4*>(p.out + token * p.ldo + static_cast<int64_t>(qh) * D + c * 32);
+        if (splits == 1) {   // to the row's place in the M tile of q, which no MMA reads any more
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             uint32_t w[4];
@@ -364,7 +412,8 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
               const __nv_bfloat162 v = __floats2bfloat162_rn(__uint_as_float(o[8 * i + 2 * h]) * inv, __uint_as_float(o[8 * i + 2 * h + 1]) * inv);
               w[h] = *reinterpret_cast<const uint32_t*>(&v);
             }
-            dst[i] = make_uint4(w[0], w[1], w[2], w[3]);
+            const int ch = c * 4 + i;
+            *reinterpret_cast<uint4*>(qt + (ch >> 3) * Cfg::kHalfTile + (((ch & 7) ^ (r & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
           }
         } else if (real) {
           uint4* dst = reinterpret_cast<uint4*>(p.part_o + part * D + c * 32);
@@ -372,15 +421,36 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
           for (int i = 0; i < 8; ++i) dst[i] = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
         }
       }
+      if (splits == 1) {   // whole rows at a time
+        __syncwarp();
+        const int64_t o_off = token * p.ldo + static_cast<int64_t>(qh) * D;
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) {
+          const int at = i * (256 / D) + lane / (D / 8), ch = lane % (D / 8), rr = (warp & 3) * 32 + at;
+          const int64_t off = __shfl_sync(0xFFFFFFFFu, o_off, at);
+          const uint4 v = *reinterpret_cast<const uint4*>(base + g * (Cfg::kQBytes / 2) + rr * 128 + (ch >> 3) * Cfg::kHalfTile + (((ch & 7) ^ (rr & 7)) << 4));
+          if (__shfl_sync(0xFFFFFFFFu, real, at)) *reinterpret_cast<uint4*>(p.out + off + ch * 8) = v;
+        }
+        __syncwarp();
+      }
       if (real && splits == 1 && p.lse != nullptr) p.lse[token * p.q_heads + qh] = inv > 0.0f ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
       if (real && splits > 1) p.part_ml[part] = make_float2(seen ? m : -INFINITY, l);
       if (splits > 1 && it.split == 0 && tid == 0) p.join[it.unit] = AttnJoin{splits, it.row0, it.n_rows, it.head, it.sq.q0};
     }
   } else if (warp < 12) {
     // ------------------------------------------------------------------ codes -> f16
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-    constexpr int kChunks = D / 16, kStep = 128 / kChunks;   // 16-code chunks of a row; rows between a thread's chunks
-    const int ct = tid - 256, c = ct % kChunks, r0 = ct / kChunks, b = c >> 1;
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kWdRegsWiden));
+    // A thread widens sixteen codes (eight with D = 64) of every eighth token, always the same channels: its rows stand
+    // alike in the swizzle, so that addresses only advance, and neither the reads nor the writes of a warp meet in a
+    // bank.  Shared-memory instructions queue behind the exponentials of the softmax warps: there are as few as can be.
+    constexpr int kCodes = D / 8, kRowsStep = 8;
+    const int ct = tid - 256, c = ct & 7, r0 = ct >> 3, b = c * kCodes / 32, half = r0 >> 3;   // rows r0 % 8 + 8 i, i of the thread's half
+    const int row_first = (r0 & 7) + half * 64;
+    const int code_at = D == 128 ? tile_offset<128>(row_first, c) : tile_offset<64>(row_first, c >> 1) + (c & 1) * 8;
+    const int ch0 = c * kCodes;   // first channel
+    const int f16_at = (ch0 >> 6) * Cfg::kHalfTile + row_first * 128;
+    const int x0 = (((ch0 >> 3) & 7) ^ (r0 & 7)) << 4, x1 = ((((ch0 >> 3) + 1) & 7) ^ (r0 & 7)) << 4;   // its 16-byte pieces
+    const bool swap = D == 128 && (c & 4) != 0;   // lanes of the second panel write theirs in the other order
     uint32_t n_step = 0;   // K and V tiles of the CTA so far: stage n_step % kWdStages
     int turn = 0;
     bool ok = true;
@@ -389,59 +459,85 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
         const int slot = turn % Cfg::kScaleSlots, there = it.end - t * kWdTile;   // tokens of the tile that count
         const uint8_t* ks = base + Cfg::kScaleAt + slot * 2 * Cfg::kScaleBytes;
         const uint8_t* vs = ks + Cfg::kScaleBytes;
-        int cs[2] = {0, 0};
+        int cs[2];
         uint32_t miss = 0;
+        bool cut = false;
 #pragma unroll
         for (int v = 0; v < 2; ++v, ++n_step) {   // K, then V
           const uint32_t st = n_step % kWdStages, phase = (n_step / kWdStages) & 1u;
-          ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&code_full[st]), phase, &abort_flag) &&
-                                           mbar_wait(smem_u32(&f16_empty[st]), phase ^ 1u, &abort_flag));
+          ok = __all_sync(0xFFFFFFFFu, mbar_wait_short(smem_u32(&code_full[st]), phase, &abort_flag) &&
+                                           mbar_wait_short(smem_u32(&f16_empty[st]), phase ^ 1u, &abort_flag));
           if (!ok) break;
-          if (v == 0) {   // the tile's exponents, in every warp: a lane has four tokens
+          if (v == 0) {
+            // the tile's exponents, in every warp (a lane has four tokens), then the factors of the thread's own token
             miss = missing[slot];
-            const bool cut = there < kWdTile || miss != 0;
+            cut = there < kWdTile || miss != 0;
+            // (the tile before is widened everywhere: its factors go)
+            named_barrier_sync(1, 128);
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
               const uint8_t* src = x == 0 ? ks : vs;
               uint32_t top = 0;
+              if (!cut) {
+                if (BL == 4) {
+                  const uint4 w = *reinterpret_cast<const uint4*>(src + lane * 16);
+                  top = __vmaxu4(__vmaxu4(w.x, w.y), __vmaxu4(w.z, w.w));
+                } else {
+                  const uint2 w = *reinterpret_cast<const uint2*>(src + lane * 8);
+                  top = __vmaxu4(w.x, w.y);
+                }
+              } else {
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                uint32_t w;
-                if (BL == 4) w = *reinterpret_cast<const uint32_t*>(src + (4 * lane + i) * 4);
-                else w = *reinterpret_cast<const uint16_t*>(src + (4 * lane + i) * 2);
-                if (cut && (4 * lane + i >= there || ((miss >> (lane >> 2)) & 1u))) w = 0;
-                top = __vmaxu4(top, w);
+                for (int i = 0; i < 4; ++i)
+                  if (4 * lane + i < there && !((miss >> (lane >> 2)) & 1u))
+                    top = __vmaxu4(top, BL == 4 ? *reinterpret_cast<const uint32_t*>(src + (4 * lane + i) * 4)
+                                                : *reinterpret_cast<const uint16_t*>(src + (4 * lane + i) * 2));
               }
               top = __vmaxu4(top, top >> 16);
               top = __reduce_max_sync(0xFFFFFFFFu, max(top & 255u, (top >> 8) & 255u));
-              cs[x] = max(static_cast<int>(top) - 127 - 7, x == 0 ? -100 : kAtMinScale);
+              const int c_tile = max(static_cast<int>(top) - 127 - 7, x == 0 ? -100 : kAtMinScale);
+              cs[x] = c_tile;
+              const uint32_t w = BL == 4 ? *reinterpret_cast<const uint32_t*>(src + ct * 4) : *reinterpret_cast<const uint16_t*>(src + ct * 2);
+#pragma unroll
+              for (int h = 0; h < BL / 2; ++h) {
+                uint32_t f = f16_pow2x2(__byte_perm(w, 0u, h == 0 ? 0x4140 : 0x4342), c_tile + 127);
+                // behind the last key (or on a page that is not there) anything may stand: values count as zero
+                if (x == 1 && cut && (ct >= there || ((miss >> (ct >> 4)) & 1u))) f = 0u;
+                uint16_t* at = &factors[x][2 * h * kWdTile + (ct & 7) * 16 + (ct >> 3)];
+                at[0] = static_cast<uint16_t>(f);
+                at[kWdTile] = static_cast<uint16_t>(f >> 16);
+              }
             }
             if (ct == 0) exponents[slot] = make_int2(cs[0], cs[1]);
+            named_barrier_sync(1, 128);
           }
-          const uint8_t* codes = base + Cfg::kCodeAt + st * Cfg::kCodeBytes;
-          uint8_t* dst = base + Cfg::kF16At + st * Cfg::kF16Bytes + (c >> 2) * Cfg::kHalfTile;
-          const uint8_t* sc = v == 0 ? ks : vs;
+          const uint8_t* codes = base + Cfg::kCodeAt + st * Cfg::kCodeBytes + code_at;
+          uint8_t* dst = base + Cfg::kF16At + st * Cfg::kF16Bytes + f16_at;
+          const uint4 fs = *reinterpret_cast<const uint4*>(&factors[v][b * kWdTile + (r0 & 7) * 16 + half * 8]);
+          const uint32_t fw[4] = {fs.x, fs.y, fs.z, fs.w};
+          auto widen = [&](auto check) {
 #pragma unroll
-          for (int i = 0; i < kChunks; ++i) {
-            const int row = r0 + i * kStep;
-            uint4 w = *reinterpret_cast<const uint4*>(codes + tile_offset<D>(row, c));
-            uint32_t f = f16_pow2(static_cast<int>(sc[row * BL + b]) - 127 - cs[v]) * 0x10001u;
-            if (v == 1 && (row >= there || ((miss >> (row >> 4)) & 1u))) {
-              // behind the last key (or on a page that is not there) anything may stand: values count as zero
-              w = make_uint4(0u, 0u, 0u, 0u);
-              f = 0u;
+            for (int i = 0; i < 8; ++i) {
+              const uint32_t f = __byte_perm(fw[i >> 1], 0u, (i & 1) ? 0x3232 : 0x1010);
+              uint8_t* line = dst + i * kRowsStep * 128;
+              if (D == 128) {
+                uint4 w = *reinterpret_cast<const uint4*>(codes + i * kRowsStep * D);
+                if (check.value && f == 0u) w = make_uint4(0u, 0u, 0u, 0u);   // not NaN times zero
+                if (swap) { uint32_t t = w.x; w.x = w.z; w.z = t; t = w.y; w.y = w.w; w.w = t; }
+                *reinterpret_cast<uint4*>(line + (swap ? x1 : x0)) = make_uint4(hmul2(e4m3x2_to_f16x2(w.x), f), hmul2(e4m3x2_to_f16x2_high(w.x), f),
+                                                                              hmul2(e4m3x2_to_f16x2(w.y), f), hmul2(e4m3x2_to_f16x2_high(w.y), f));
+                *reinterpret_cast<uint4*>(line + (swap ? x0 : x1)) = make_uint4(hmul2(e4m3x2_to_f16x2(w.z), f), hmul2(e4m3x2_to_f16x2_high(w.z), f),
+                                                                              hmul2(e4m3x2_to_f16x2(w.w), f), hmul2(e4m3x2_to_f16x2_high(w.w), f));
+              } else {
+                uint2 w = *reinterpret_cast<const uint2*>(codes + i * kRowsStep * D);
+                if (check.value && f == 0u) w = make_uint2(0u, 0u);
+                *reinterpret_cast<uint4*>(line + x0) = make_uint4(hmul2(e4m3x2_to_f16x2(w.x), f), hmul2(e4m3x2_to_f16x2_high(w.x), f),
+                                                                 hmul2(e4m3x2_to_f16x2(w.y), f), hmul2(e4m3x2_to_f16x2_high(w.y), f));
+              }
             }
-            const uint4 lo = make_uint4(hmul2(e4m3x2_to_f16x2(w.x), f), hmul2(e4m3x2_to_f16x2_high(w.x), f),
-                                        hmul2(e4m3x2_to_f16x2(w.y), f), hmul2(e4m3x2_to_f16x2_high(w.y), f));
-            const uint4 hi = make_uint4(hmul2(e4m3x2_to_f16x2(w.z), f), hmul2(e4m3x2_to_f16x2_high(w.z), f),
-                                        hmul2(e4m3x2_to_f16x2(w.w), f), hmul2(e4m3x2_to_f16x2_high(w.w), f));
-            // the second panel's lanes write their halves in the other order: no two of eight lanes meet in a bank
-            const bool swap = (c & 4) != 0;
-            const int at = (c & 3) * 2;
-            uint8_t* line = dst + row * 128;
-            *reinterpret_cast<uint4*>(line + (((at + (swap ? 1 : 0)) ^ (row & 7)) << 4)) = swap ? hi : lo;
-            *reinterpret_cast<uint4*>(line + (((at + (swap ? 0 : 1)) ^ (row & 7)) << 4)) = swap ? lo : hi;
-          }
+          };
+          if (v == 1 && cut) widen(std::true_type{});
+          else widen(std::false_type{});
           fence_proxy_async_smem();
           __syncwarp();
           if (lane == 0) {
@@ -452,7 +548,7 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
       }
     }
   } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kWdRegsIssue));
     if (warp == 12) {
       // ---------------------------------------------------------------- codes and scales by TMA
       const int box = min(1 << p.page_shift, 32), boxes = kWdTile / box;   // rows of a copy; copies of a tile
@@ -478,7 +574,7 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
 #pragma unroll
           for (int v = 0; v < 2; ++v, ++n_step) {
             const uint32_t st = n_step % kWdStages, phase = (n_step / kWdStages) & 1u;
-            ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&code_empty[st]), phase ^ 1u, &abort_flag));
+            ok = __all_sync(0xFFFFFFFFu, mbar_wait_short(smem_u32(&code_empty[st]), phase ^ 1u, &abort_flag));
             if (!ok) break;
             const uint32_t bar = smem_u32(&code_full[st]);
             if (lane == 0) {
@@ -522,7 +618,7 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
       uint32_t n_step = 0, q_phase[2] = {0, 0}, p_phase[2] = {0, 0};
       bool ok = true;
       auto wait = [&](uint64_t* bar, uint32_t phase) {
-        ok = ok && __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(bar), phase, &abort_flag));
+        ok = ok && __all_sync(0xFFFFFFFFu, mbar_wait_short(smem_u32(bar), phase, &abort_flag));
         return ok;
       };
       auto scores = [&](int g, uint32_t st) {
@@ -557,10 +653,10 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
             if (g == 0 && !wait(&f16_full[vst], (vn / kWdStages) & 1u)) break;
             tc_fence_after_sync();
             if (elect_one()) {
+              const uint64_t v = v_desc + static_cast<uint32_t>((vst * Cfg::kF16Bytes) >> 4);
 #pragma unroll
               for (int kk = 0; kk < kWdTile / 16; ++kk)
-                tc_mma_f16_ta(tmem + 256 + g * 128, tmem + g * 128 + kk * 8, v_desc + static_cast<uint32_t>((vst * Cfg::kF16Bytes + kk * 2048) >> 4),
-                              idesc_o, j > 0 || kk > 0);
+                tc_mma_f16_ta(tmem + 256 + g * 128, tmem + g * 128 + kk * 8, v + static_cast<uint32_t>((kk * 2048) >> 4), idesc_o, j > 0 || kk > 0);
               if (g == groups - 1) tc_commit(smem_u32(&f16_empty[vst]));
               if (j == n - 1) tc_commit(smem_u32(&o_done[g]));
             }
@@ -589,7 +685,7 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
   __syncthreads();
   if (warp == 13) {
     tc_fence_after_sync();
-    tmem_dealloc(tmem, 512);
+    tmem_dealloc(tmem_base_smem, 512);
   }
 }
 
