@@ -303,8 +303,8 @@ batq_status batq_linear_w4a4_noalloc(const batq_transform* t, const batq_weight*
  *   k_scales, v_scales  [pages][kv_heads][page_size][head_dim / 32] bytes,
  * dense, 16-byte aligned, which outlive it.  Nothing is allocated on the device and nothing is written: several
  * handles may name the same buffers.  Slot s is token s % page_size of page s / page_size.
- *   page_size 16, 32, 64 or 128; head_dim 64 or 128 (else UNSUPPORTED); pages * kv_heads * page_size < 2^31 (else
- *   SHAPE). */
+ *   page_size 16, 32, 64 or 128; head_dim 64 or 128 (else UNSUPPORTED); kv_heads (and q_heads below) <= 32768,
+ *   pages * kv_heads * page_size < 2^31 (else SHAPE). */
 batq_status batq_kv_cache_create(batq_kv_cache** out, void* k_codes, void* k_scales, void* v_codes, void* v_scales,
                                  int64_t pages, int32_t page_size, int32_t kv_heads, int32_t head_dim);
 batq_status batq_kv_cache_destroy(batq_kv_cache* c);

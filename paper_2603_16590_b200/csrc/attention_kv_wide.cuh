@@ -108,12 +108,6 @@ __device__ __forceinline__ uint32_t f16x2_pack(float lo, float hi) {
   return r;
 }
 
-// 16 bytes global -> shared, the rest behind `bytes` as zeros; waiting for all of the thread's.
-__device__ __forceinline__ void cp_async_16(uint32_t dst_smem, const void* src, int bytes) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst_smem), "l"(src), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ void cp_async_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
-
 // One part of a unit.
 struct AttnWideItem {
   AttnSeq sq;
@@ -271,7 +265,8 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
           cp_async_16(smem_u32(base + g * (Cfg::kQBytes / 2) + rr * 128 + (ch >> 3) * Cfg::kHalfTile + (((ch & 7) ^ (rr & 7)) << 4)),
                       p.q + (there ? off : 0) + ch * 8, there ? 16 : 0);
         }
-        cp_async_wait_all();
+        cp_async_commit();
+        cp_async_wait<0>();
         __syncwarp();
         float amax = 0.0f;
 #pragma unroll
