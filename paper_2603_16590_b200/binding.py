@@ -113,7 +113,8 @@ def load():
         for name, (res, args) in SIGNATURES.items():
             fn = getattr(lib, name)
             fn.restype, fn.argtypes = res, args
-        for name in ("batq_linear_w4a4", "batq_linear_w4a8", "batq_quantize_act", "batq_quantize_act_mxfp8"):
+        for name in ("batq_linear_w4a4", "batq_linear_w4a8", "batq_quantize_act", "batq_quantize_act_mxfp8", "batq_kv_append_mxfp8",
+                     "batq_attention_kv_mxfp8"):
             _ADDRESS[name] = C.cast(getattr(lib, name), _P).value
         _CALL = _load_call_shim()
         _LIB = lib   # last: another thread may be in a call
@@ -132,7 +133,7 @@ def _load_call_shim():
     loader = importlib.machinery.ExtensionFileLoader("_pycall", path)
     shim = importlib.util.module_from_spec(importlib.util.spec_from_loader("_pycall", loader))
     loader.exec_module(shim)
-    shim.setup(torch.float32, torch.Tensor)
+    shim.setup(torch.float32, torch.Tensor, torch.bfloat16, torch.int32, torch.int64)
     return shim
 
 
@@ -454,16 +455,45 @@ def batq_kv_cache_create(k_codes, k_scales, v_codes, v_scales) -> KVCache:
     return KVCache(k_codes, k_scales, v_codes, v_scales)
 
 
+def _vector(x, dtype, n, what):
+    """The kernels read n entries of these: a shorter tensor, or one of another type, would be read past its end."""
+    if x is not None and (x.dtype is not dtype or x.dim() != 1 or x.size(0) < n or (n > 1 and x.stride(0) != 1)):
+        raise ValueError(f"{what}: a dense {dtype} vector of {n} entries")
+
+
+def _rows(x, tokens, width, what):
+    if x.dtype is not torch.bfloat16 or x.dim() != 2 or x.size(0) < tokens or (x.size(1) != width if width else x.size(1) == 0) or (
+            x.stride(1) != 1 and x.size(1) > 1):
+        raise ValueError(f"{what}: bf16 rows, {tokens} of them" + (f", {width} wide" if width else ""))
+
+
 def batq_kv_append_mxfp8(cache: KVCache, t_k, t_v, k, v, slots, positions=None, rope=None, t_q=None, q=None, q_out=None):
     """k, v, q: bf16 [tokens, heads * head_dim] with any row stride; slots int64, positions int32 [tokens]; rope fp32
     [rows, rot_dim], cosines then sines."""
-    tokens = k.shape[0]
-    with_q = q is not None
-    st = load().batq_kv_append_mxfp8(
-        cache.handle, t_k.handle if t_k else None, t_v.handle if t_v else None, t_q.handle if t_q else None, _ptr(k), k.stride(0),
-        _ptr(v), v.stride(0), _ptr(q), q.stride(0) if with_q else 0, _ptr(q_out), q_out.stride(0) if q_out is not None else 0,
-        q.shape[1] // cache.head_dim if with_q else 0, tokens, _ptr(slots), _ptr(positions), _ptr(rope),
-        rope.shape[0] if rope is not None else 0, rope.shape[1] if rope is not None else 0, _stream())
+    if _LIB is None:
+        load()
+    if _CALL is not None:
+        st = _CALL.kv_append(_ADDRESS["batq_kv_append_mxfp8"], _handle(cache), cache.kv_heads, cache.head_dim, _handle(t_k), _handle(t_v),
+                             _handle(t_q), k, v, q, q_out, slots, positions, rope, _stream())
+    else:
+        tokens, width = k.size(0), cache.kv_heads * cache.head_dim
+        _rows(k, tokens, width, "k")
+        _rows(v, tokens, width, "v")
+        _vector(slots, torch.int64, tokens, "slots")
+        _vector(positions, torch.int32, tokens, "positions")
+        if q is not None and q_out is not None:
+            _rows(q, tokens, 0, "q")
+            _rows(q_out, tokens, q.size(1), "q_out")
+            if q.size(1) % cache.head_dim:
+                raise ValueError("q: whole heads")
+        if rope is not None and (rope.dtype is not torch.float32 or not rope.is_contiguous() or rope.dim() != 2):
+            raise ValueError("rope: a dense float32 table")
+        with_q, with_out, with_rope = q is not None, q_out is not None, rope is not None
+        st = _LIB.batq_kv_append_mxfp8(
+            _handle(cache), _handle(t_k), _handle(t_v), _handle(t_q), _ptr(k), k.stride(0), _ptr(v), v.stride(0), _ptr(q),
+            q.stride(0) if with_q else 0, _ptr(q_out), q_out.stride(0) if with_out else 0, q.shape[1] // cache.head_dim if with_q else 0,
+            k.shape[0], _ptr(slots), _ptr(positions), _ptr(rope), rope.shape[0] if with_rope else 0, rope.shape[1] if with_rope else 0,
+            _stream())
     _check(st, "batq_kv_append_mxfp8")
 
 
@@ -475,10 +505,28 @@ def batq_attention_kv_mxfp8(cache: KVCache, q, out, kv_lens, page_table, max_q, 
                             causal=True, lse=None):
     """q, out: bf16 [tokens, q_heads * head_dim] with any row stride; kv_lens int32 [seqs]; page_table int32 [seqs, pages];
     q_starts int32 [seqs + 1], None: one row per sequence; scale None: head_dim ** -0.5."""
-    st = load().batq_attention_kv_mxfp8(
-        cache.handle, _ptr(q), q.stride(0), q.shape[1] // cache.head_dim, q.shape[0], _ptr(q_starts), _ptr(kv_lens), _ptr(page_table),
-        page_table.stride(0), kv_lens.shape[0], max_q, max_kv, cache.head_dim ** -0.5 if scale is None else scale, 1 if causal else 0,
-        _ptr(out), out.stride(0), _ptr(lse), _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream())
+    if _LIB is None:
+        load()
+    scale = cache.head_dim ** -0.5 if scale is None else scale
+    if _CALL is not None:
+        st = _CALL.attention(_ADDRESS["batq_attention_kv_mxfp8"], _handle(cache), cache.head_dim, q, out, kv_lens, page_table, max_q, max_kv,
+                             workspace, q_starts, scale, 1 if causal else 0, lse, _stream())
+    else:
+        tokens, seqs = q.size(0), kv_lens.size(0)
+        _rows(q, tokens, 0, "q")
+        _rows(out, tokens, q.size(1), "out")
+        _vector(kv_lens, torch.int32, seqs, "kv_lens")
+        _vector(q_starts, torch.int32, seqs + 1, "q_starts")
+        if page_table.dtype is not torch.int32 or page_table.dim() != 2 or page_table.size(0) < seqs or not page_table.is_contiguous():
+            raise ValueError("page_table: dense int32, a row per sequence")
+        if q.size(1) % cache.head_dim:
+            raise ValueError("q: whole heads")
+        if lse is not None and (lse.dtype is not torch.float32 or not lse.is_contiguous() or lse.numel() < tokens * (q.size(1) // cache.head_dim)):
+            raise ValueError("lse: dense float32, [tokens, q_heads]")
+        st = _LIB.batq_attention_kv_mxfp8(
+            _handle(cache), _ptr(q), q.stride(0), q.shape[1] // cache.head_dim, q.shape[0], _ptr(q_starts), _ptr(kv_lens), _ptr(page_table),
+            page_table.shape[1], kv_lens.shape[0], max_q, max_kv, scale, 1 if causal else 0, _ptr(out), out.stride(0), _ptr(lse),
+            _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream())
     _check(st, "batq_attention_kv_mxfp8")
 
 

@@ -287,7 +287,7 @@ def test_attention_refuses(batq):
     _refused(batq, SHAPE, lambda: call(max_q=0))
     _refused(batq, SHAPE, lambda: call(max_kv=-1))
     _refused(batq, SHAPE, lambda: call(scale=math.nan))
-    _refused(batq, SHAPE, lambda: call(q=q[:, :384]))                    # 3 heads over 2
+    _refused(batq, SHAPE, lambda: call(q=q[:, :384], out=out[:, :384]))                    # 3 heads over 2
     _refused(batq, SHAPE, lambda: call(q=torch.zeros(1024, dtype=torch.bfloat16, device="cuda").expand(5, 1024)))
     _refused(batq, ALIGN, lambda: call(q=torch.zeros(5, 1028, dtype=torch.bfloat16, device="cuda")[:, :1024]))
     _refused(batq, ALIGN, lambda: call(out=torch.zeros(5, 1032, dtype=torch.bfloat16, device="cuda")[:, 4:1028]))
@@ -508,7 +508,7 @@ def test_append_refuses(batq):
     _refused(batq, SHAPE, lambda: call(rope=torch.zeros(400, 24, device="cuda")))
     _refused(batq, SHAPE, lambda: call(rope=torch.zeros(400, 256, device="cuda")))
     _refused(batq, SHAPE, lambda: call(rope=rope[:9], pos=None))                         # fewer rows than tokens
-    _refused(batq, SHAPE, lambda: call(k=torch.zeros(128, dtype=torch.bfloat16, device="cuda").expand(10, 128)))
+    _refused(batq, SHAPE, lambda: call(k=torch.zeros(256, dtype=torch.bfloat16, device="cuda").expand(10, 256)))
     _refused(batq, ALIGN, lambda: call(v=torch.zeros(10, 264, dtype=torch.bfloat16, device="cuda")[:, 4:260]))
     _refused(batq, ALIGN, lambda: call(k=torch.zeros(10, 260, dtype=torch.bfloat16, device="cuda")[:, :256]))
     mid = _transforms(batq, 128, 4, 8, 1)[1]

@@ -82,3 +82,85 @@ def test_reference_attention_by_hand():
     assert abs(out[1, 0, 3] - (4 * e + 8 * e * e) / (e + e * e)) < 1e-12 and abs(lse[1, 0] - np.log(e + e * e)) < 1e-12
     out, lse, _ = R.attention(q, R.mxfp8(k), R.mxfp8(v), [2], [1], [[1]], 1.0, True)
     assert out[0].abs().max() == 0 and lse[0, 0] == -np.inf and abs(out[1, 0, 3] - 4) < 1e-12
+
+
+# ------------------------------------------------------------------------------------------------ the binding
+class _Cache:
+    handle = C.c_void_p(64)
+    kv_heads, head_dim = 2, 64
+
+
+def _call_arguments(monkeypatch, shim):
+    """What the two calls hand to their C entry points: through the shim, or through ctypes."""
+    seen = []
+    P, I64, I32, SZ, F = C.c_void_p, C.c_int64, C.c_int32, C.c_size_t, C.c_float
+    append = C.CFUNCTYPE(C.c_int, P, P, P, P, P, I64, P, I64, P, I64, P, I64, I32, I64, P, P, P, I64, I32, P)(lambda *a: seen.append(a) or 0)
+    attend = C.CFUNCTYPE(C.c_int, P, P, I64, I32, I64, P, P, P, I64, I32, I32, I32, F, I32, P, I64, P, P, SZ, P)(lambda *a: seen.append(a) or 0)
+    if shim:
+        monkeypatch.setattr(binding, "_ADDRESS", {"batq_kv_append_mxfp8": C.cast(append, P).value, "batq_attention_kv_mxfp8": C.cast(attend, P).value})
+    else:
+        monkeypatch.setattr(binding, "_CALL", None)
+        monkeypatch.setattr(binding, "_LIB", type("Lib", (), {"batq_kv_append_mxfp8": staticmethod(append), "batq_attention_kv_mxfp8": staticmethod(attend)}))
+    monkeypatch.setattr(binding, "_stream", lambda: 7)
+    x = torch.zeros(5, 640, dtype=torch.bfloat16)
+    q, k, v = x.split([384, 128, 128], 1)
+    q_out = torch.zeros(5, 400, dtype=torch.bfloat16)[:, :384]
+    slots, pos, rope = torch.zeros(5, dtype=torch.int64), torch.zeros(5, dtype=torch.int32), torch.zeros(9, 32)
+    t = type("T", (), {"handle": C.c_void_p(32)})()
+    binding.batq_kv_append_mxfp8(_Cache, t, None, k, v, slots, positions=pos, rope=rope, t_q=t, q=q, q_out=q_out)
+    binding.batq_kv_append_mxfp8(_Cache, None, t, k, v, slots)
+    lens, table, starts = torch.zeros(3, dtype=torch.int32), torch.zeros(3, 11, dtype=torch.int32), torch.zeros(4, dtype=torch.int32)
+    lse, ws = torch.zeros(5, 6), torch.zeros(512, dtype=torch.uint8)
+    binding.batq_attention_kv_mxfp8(_Cache, q, q_out, lens, table, 4, 99, ws, q_starts=starts, scale=0.5, causal=False, lse=lse)
+    binding.batq_attention_kv_mxfp8(_Cache, q[:3], q_out[:3], lens, table, 1, 99)
+    ptr = lambda a: a.data_ptr()  # noqa: E731
+    assert seen == [
+        (64, 32, None, 32, ptr(k), 640, ptr(v), 640, ptr(q), 640, ptr(q_out), 400, 6, 5, ptr(slots), ptr(pos), ptr(rope), 9, 32, 7),
+        (64, None, 32, None, ptr(k), 640, ptr(v), 640, None, 0, None, 0, 0, 5, ptr(slots), None, None, 0, 0, 7),
+        (64, ptr(q), 640, 6, 5, ptr(starts), ptr(lens), ptr(table), 11, 3, 4, 99, 0.5, 0, ptr(q_out), 400, ptr(lse), ptr(ws), 512, 7),
+        (64, ptr(q), 640, 6, 3, None, ptr(lens), ptr(table), 11, 3, 1, 99, 0.125, 1, ptr(q_out), 400, None, None, 0, 7)]
+
+
+def test_arguments_through_the_shim(lib, monkeypatch):
+    assert binding._CALL is not None
+    _call_arguments(monkeypatch, True)
+
+
+def test_arguments_through_ctypes(lib, monkeypatch):
+    _call_arguments(monkeypatch, False)
+
+
+@pytest.mark.parametrize("shim", [True, False])
+def test_tensors_of_another_form_are_refused(lib, monkeypatch, shim):
+    """What the kernels would read or write past an end of: refused before the library is called."""
+    monkeypatch.setattr(binding, "_stream", lambda: 7)
+    called = []
+    P, I64, I32, SZ, F = C.c_void_p, C.c_int64, C.c_int32, C.c_size_t, C.c_float
+    append = C.CFUNCTYPE(C.c_int, P, P, P, P, P, I64, P, I64, P, I64, P, I64, I32, I64, P, P, P, I64, I32, P)(lambda *a: called.append(a) or 0)
+    attend = C.CFUNCTYPE(C.c_int, P, P, I64, I32, I64, P, P, P, I64, I32, I32, I32, F, I32, P, I64, P, P, SZ, P)(lambda *a: called.append(a) or 0)
+    monkeypatch.setattr(binding, "_ADDRESS", {"batq_kv_append_mxfp8": C.cast(append, P).value, "batq_attention_kv_mxfp8": C.cast(attend, P).value})
+    if not shim:
+        monkeypatch.setattr(binding, "_CALL", None)
+    monkeypatch.setattr(binding, "_LIB", type("Lib", (), {"batq_kv_append_mxfp8": staticmethod(lambda *a: called.append(a) or 0),
+                                                          "batq_attention_kv_mxfp8": staticmethod(lambda *a: called.append(a) or 0)}))
+    x = torch.zeros(5, 640, dtype=torch.bfloat16)
+    q, k, v = x.split([384, 128, 128], 1)
+    slots, pos, rope = torch.zeros(5, dtype=torch.int64), torch.zeros(5, dtype=torch.int32), torch.zeros(9, 32)
+    good = dict(positions=pos, rope=rope, q=q, q_out=q)
+    binding.batq_kv_append_mxfp8(_Cache, None, None, k, v, slots, **good)
+    for bad in (dict(slots=slots[:4]), dict(slots=slots.int()), dict(slots=torch.zeros(10, dtype=torch.int64)[::2]), dict(positions=pos[:4]),
+                dict(positions=pos.long()), dict(rope=rope.double()), dict(rope=rope[:, :16]), dict(k=k[:, :64]), dict(k=k.float()),
+                dict(v=v[:4]), dict(q_out=q[:4]), dict(q_out=q[:, :320]), dict(q=q[:, :100], q_out=q[:, :100]),
+                dict(k=torch.zeros(128, 5, dtype=torch.bfloat16).t())):
+        with pytest.raises(ValueError):
+            a = {**dict(k=k, v=v, slots=slots), **good, **bad}
+            binding.batq_kv_append_mxfp8(_Cache, None, None, a.pop("k"), a.pop("v"), a.pop("slots"), **a)
+    lens, table, starts = torch.zeros(3, dtype=torch.int32), torch.zeros(3, 11, dtype=torch.int32), torch.zeros(4, dtype=torch.int32)
+    good = dict(q=q, out=q, kv_lens=lens, page_table=table, max_q=4, max_kv=99, q_starts=starts)
+    binding.batq_attention_kv_mxfp8(_Cache, **good)
+    for bad in (dict(q=q.float()), dict(out=q[:4]), dict(out=q[:, :320]), dict(kv_lens=lens.long()), dict(q_starts=starts[:3]),
+                dict(q_starts=starts.long()), dict(page_table=table[:2]), dict(page_table=table.long()), dict(page_table=table[:, :5]),
+                dict(lse=torch.zeros(4, 6)), dict(lse=torch.zeros(5, 6).double()), dict(q=q[:, :100], out=q[:, :100])):
+        with pytest.raises(ValueError):
+            binding.batq_attention_kv_mxfp8(_Cache, **{**good, **bad})
+    assert len(called) == 2
