@@ -28,26 +28,43 @@
 
 namespace batq {
 
-constexpr int kWdThreads = 512;
 constexpr int kWdRows = 256;        // of a unit
 constexpr int kWdTile = 128;        // tokens
-constexpr int kWdStages = 3;        // of codes, and of f16 tiles
-// Registers of a thread of the softmax warps (which hold 128 scores), the widening ones and the others.
-constexpr int kWdRegsSoftmax = 192, kWdRegsWiden = 80, kWdRegsIssue = 48;
-static_assert(256 * kWdRegsSoftmax + 128 * kWdRegsWiden + 128 * kWdRegsIssue <= 65536, "what the block is launched with: 128 each");
 constexpr int kWdPartCost = 4;      // what a part of a unit costs besides its tiles, in tiles
 
 struct AttnWidePlan { int32_t units, splits; };
 
+// READY: the tiles come widened from the workspace (attention_widen_kernel), not from the cache.
+template <int D, bool READY>
+struct AttnWideShape {
+  static constexpr int kThreads = READY ? 384 : 512;
+  static constexpr int kStages = READY ? 4 : 3;   // f16 tiles; and of codes
+  static constexpr int kIssueWarp = READY ? 8 : 12;
+  // Registers of a thread of the softmax warps (which hold 128 scores), the widening ones and the others.
+  static constexpr int kRegs = READY ? 168 : 128, kRegsSoftmax = READY ? 208 : 192, kRegsWiden = 80, kRegsIssue = READY ? 80 : 48;
+  static_assert(256 * kRegsSoftmax + (READY ? 0 : 128 * kRegsWiden) + 128 * kRegsIssue <= kThreads * kRegs, "what the block is launched with");
+};
+
+// What the softmax has to know of a tile.
+struct AttnTileInfo {
+  int32_t ck, cv;       // the exponents that its keys and values have been divided by
+  uint32_t missing;     // 16-token pieces of it whose page is not there
+  int32_t pad;
+};
+
 struct AttnWideParams {
   AttnParams a;
+  uint8_t* tiles;        // READY: [sequence][head][tile][K, V], each as it stands in shared memory
+  AttnTileInfo* info;    //        [sequence][head][tile]
+  int32_t max_tiles;     //        of a sequence
   int32_t least_rows;   // sequences with fewer rows are attention_kv_kernel's
   int32_t max_items;    // parts of units that the workspace has room for
   AttnWidePlan* plan;   // written by the first CTA for the join; part_o, part_ml: [item][256 rows], join: [unit]
 };
 
-template <int D>
+template <int D, bool READY>
 struct AttnWideCfg {
+  using Shape = AttnWideShape<D, READY>;
   static constexpr int kBlocks = D / 32;
   static constexpr int kPanels = D / 64;                         // 64-channel halves of a row: 128 bytes of f16
   static constexpr int kHalfTile = 128 * 128;                    // 128 rows of one panel
@@ -56,8 +73,8 @@ struct AttnWideCfg {
   static constexpr int kCodeBytes = kWdTile * D;
   static constexpr int kScaleBytes = kWdTile * kBlocks;          // of K or V
   static constexpr int kScaleSlots = 4;
-  static constexpr int kF16At = kQBytes, kCodeAt = kF16At + kWdStages * kF16Bytes, kScaleAt = kCodeAt + kWdStages * kCodeBytes;
-  static constexpr int kSmemBytes = kScaleAt + kScaleSlots * 2 * kScaleBytes + 1024;
+  static constexpr int kF16At = kQBytes, kCodeAt = kF16At + Shape::kStages * kF16Bytes, kScaleAt = kCodeAt + Shape::kStages * kCodeBytes;
+  static constexpr int kSmemBytes = (READY ? kCodeAt : kScaleAt + kScaleSlots * 2 * kScaleBytes) + 1024;
 };
 
 // As f16_idesc_bf16 with f16 operands; b_mn: B is MN-major.
@@ -116,22 +133,22 @@ struct AttnWideItem {
   int tile0, tile1;
 };
 
-template <int D>
-__global__ void __launch_bounds__(kWdThreads, 1)
+template <int D, bool READY>
+__global__ void __launch_bounds__(AttnWideShape<D, READY>::kThreads, 1)
 attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
                          const __grid_constant__ AttnWideParams wp) {
-  using Cfg = AttnWideCfg<D>;
-  constexpr int BL = Cfg::kBlocks;
+  using Cfg = AttnWideCfg<D, READY>;
+  using Shape = AttnWideShape<D, READY>;
+  constexpr int BL = Cfg::kBlocks, kStages = Shape::kStages;
   const AttnParams& p = wp.a;
   extern __shared__ __align__(1024) uint8_t wd_smem[];
-  __shared__ __align__(8) uint64_t code_full[kWdStages], code_empty[kWdStages], f16_full[kWdStages], f16_empty[kWdStages];
+  __shared__ __align__(8) uint64_t code_full[kStages], code_empty[kStages], f16_full[kStages], f16_empty[kStages];
   __shared__ __align__(8) uint64_t s_full[2], p_ready[2], o_done[2], q_ready[2], drain;
   __shared__ int first[kAtMaxSeqs];   // units in front of each sequence's
-  __shared__ int scan_sum[kWdThreads / 32], scan_max[kWdThreads / 32];
-  __shared__ int2 exponents[Cfg::kScaleSlots];   // (ck, cv) of a tile
-  __shared__ uint32_t missing[Cfg::kScaleSlots]; // 16-token pieces of a tile whose page is not there
+  __shared__ int scan_sum[Shape::kThreads / 32], scan_max[Shape::kThreads / 32];
+  __shared__ __align__(16) AttnTileInfo info[Cfg::kScaleSlots];
   // 2^(e - c) of a tile's keys, values: f16, [block][token % 8][token / 8], so that a widening thread's are one run
-  __shared__ __align__(16) uint16_t factors[2][kWdTile * BL];
+  __shared__ __align__(16) uint16_t factors[READY ? 1 : 2][READY ? 1 : kWdTile * BL];
   __shared__ uint32_t tmem_base_smem;
   __shared__ int abort_flag;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -139,10 +156,10 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
 
   grid_launch_dependents();
   if (tid == 0) {
-    for (int i = 0; i < kWdStages; ++i) {
+    for (int i = 0; i < kStages; ++i) {
       mbar_init(smem_u32(&code_full[i]), 1);
       mbar_init(smem_u32(&code_empty[i]), 4);
-      mbar_init(smem_u32(&f16_full[i]), 4);
+      mbar_init(smem_u32(&f16_full[i]), READY ? 1 : 4);
       mbar_init(smem_u32(&f16_empty[i]), 1);
     }
     for (int i = 0; i < 2; ++i) {
@@ -154,10 +171,12 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
     mbar_init(smem_u32(&drain), 1);
     mbar_fence_init();
     abort_flag = 0;
-    tma_prefetch_desc(&tmap_k);
-    tma_prefetch_desc(&tmap_v);
+    if (!READY) {
+      tma_prefetch_desc(&tmap_k);
+      tma_prefetch_desc(&tmap_v);
+    }
   }
-  if (warp == 13) {
+  if (warp == Shape::kIssueWarp + 1) {
     tmem_alloc(smem_u32(&tmem_base_smem), 512);
     tmem_relinquish();
   }
@@ -166,15 +185,19 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
   // units of each sequence, of all, and the most tiles of one
   int units, splits;
   {
-    const int s = tid;   // kAtMaxSeqs == kWdThreads
-    int mine = 0, tiles = 0;
-    if (s < p.seqs) {
-      const AttnSeq q = attn_seq(p, s);
-      const int rows = q.nq * p.group;
-      mine = rows >= wp.least_rows ? p.kv_heads * ((rows + kWdRows - 1) / kWdRows) : 0;
-      tiles = mine > 0 ? (q.len + kWdTile - 1) / kWdTile : 0;
+    int mine[2] = {0, 0}, tiles = 0;   // two sequences a thread
+    static_assert(kAtMaxSeqs <= 2 * 256, "");
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int s = 2 * tid + i;
+      if (s < p.seqs) {
+        const AttnSeq q = attn_seq(p, s);
+        const int rows = q.nq * p.group;
+        mine[i] = rows >= wp.least_rows ? p.kv_heads * ((rows + kWdRows - 1) / kWdRows) : 0;
+        if (mine[i] > 0) tiles = max(tiles, (q.len + kWdTile - 1) / kWdTile);
+      }
     }
-    int scan = mine;
+    int scan = mine[0] + mine[1];
 #pragma unroll
     for (int x = 1; x < 32; x <<= 1) {
       const int v = __shfl_up_sync(0xFFFFFFFFu, scan, x);
@@ -186,14 +209,17 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
-    int before = scan - mine;
+    int before = scan - mine[0] - mine[1];
     units = tiles = 0;
-    for (int w = 0; w < kWdThreads / 32; ++w) {
+    for (int w = 0; w < Shape::kThreads / 32; ++w) {
       if (w < warp) before += scan_sum[w];
       units += scan_sum[w];
       tiles = max(tiles, scan_max[w]);
     }
-    first[s] = before;
+    if (2 * tid < kAtMaxSeqs) {
+      first[2 * tid] = before;
+      first[2 * tid + 1] = before + mine[0];
+    }
     __syncthreads();
     splits = 1;
     int best = INT_MAX;
@@ -237,7 +263,7 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
   AttnWideItem it;
   if (warp < 8) {
     // ------------------------------------------------------------------ softmax: thread = row
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kWdRegsSoftmax));
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(Shape::kRegsSoftmax));
     const int g = warp >> 2, r = tid & 127;
     const uint32_t lanes = static_cast<uint32_t>(warp & 3) << 21;   // tensor memory lanes of this warp
     const uint32_t s_at = tmem + lanes + g * 128, o_at = tmem + lanes + 256 + g * 128;
@@ -301,8 +327,8 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
         if (!ok) break;
         s_phase ^= 1u;
         tc_fence_after_sync();
-        const int2 ex = exponents[(turn + j) % Cfg::kScaleSlots];
-        const uint32_t miss = missing[(turn + j) % Cfg::kScaleSlots];
+        const AttnTileInfo ex = info[(turn + j) % Cfg::kScaleSlots];
+        const uint32_t miss = ex.missing;
         const int tok0 = (it.tile0 + j) * kWdTile, see = lim - tok0;
         const bool part = tok0 + kWdTile > full || miss != 0;
         uint32_t s[4][32];
@@ -332,7 +358,7 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
           for (int i = 1; i < 32; ++i) tops[c] = fmaxf(tops[c], __uint_as_float(s[c][i]));
         }
         const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-        const float qk = fmaxf(qs * pow2i(max(ex.x, -126)), 1e-37f), cv = static_cast<float>(ex.y);
+        const float qk = fmaxf(qs * pow2i(max(ex.ck, -126)), 1e-37f), cv = static_cast<float>(ex.cv);
         if (__any_sync(0xFFFFFFFFu, fmaf(top, qk, cv - m) > kAtSlack)) {
           const float mn = fmaxf(m, fmaf(top, qk, cv)), alpha = ex2(m - mn);
           m = mn;
@@ -369,7 +395,7 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
         }
         float a, b;
         f32x2_unpack(f32x2_add(sum0, sum1), a, b);
-        l = fmaf(a + b, pow2i(max(-ex.y, -126)), l);
+        l = fmaf(a + b, pow2i(max(-ex.cv, -126)), l);
         tmem_st_wait();
         tc_fence_before_sync();
         __syncwarp();
@@ -432,9 +458,9 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
       if (real && splits > 1) p.part_ml[part] = make_float2(seen ? m : -INFINITY, l);
       if (splits > 1 && it.split == 0 && tid == 0) p.join[it.unit] = AttnJoin{splits, it.row0, it.n_rows, it.head, it.sq.q0};
     }
-  } else if (warp < 12) {
+  } else if (!READY && warp < 12) {
     // ------------------------------------------------------------------ codes -> f16
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kWdRegsWiden));
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Shape::kRegsWiden));
     // A thread widens sixteen codes (eight with D = 64) of every eighth token, always the same channels: its rows stand
     // alike in the swizzle, so that addresses only advance, and neither the reads nor the writes of a warp meet in a
     // bank.  Shared-memory instructions queue behind the exponentials of the softmax warps: there are as few as can be.
@@ -446,7 +472,7 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
     const int f16_at = (ch0 >> 6) * Cfg::kHalfTile + row_first * 128;
     const int x0 = (((ch0 >> 3) & 7) ^ (r0 & 7)) << 4, x1 = ((((ch0 >> 3) + 1) & 7) ^ (r0 & 7)) << 4;   // its 16-byte pieces
     const bool swap = D == 128 && (c & 4) != 0;   // lanes of the second panel write theirs in the other order
-    uint32_t n_step = 0;   // K and V tiles of the CTA so far: stage n_step % kWdStages
+    uint32_t n_step = 0;   // K and V tiles of the CTA so far: stage n_step % kStages
     int turn = 0;
     bool ok = true;
     for (int k = 0; ok && item_at(k, &it); ++k) {
@@ -459,13 +485,13 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
         bool cut = false;
 #pragma unroll
         for (int v = 0; v < 2; ++v, ++n_step) {   // K, then V
-          const uint32_t st = n_step % kWdStages, phase = (n_step / kWdStages) & 1u;
+          const uint32_t st = n_step % kStages, phase = (n_step / kStages) & 1u;
           ok = __all_sync(0xFFFFFFFFu, mbar_wait_short(smem_u32(&code_full[st]), phase, &abort_flag) &&
                                            mbar_wait_short(smem_u32(&f16_empty[st]), phase ^ 1u, &abort_flag));
           if (!ok) break;
           if (v == 0) {
             // the tile's exponents, in every warp (a lane has four tokens), then the factors of the thread's own token
-            miss = missing[slot];
+            miss = info[slot].missing;
             cut = there < kWdTile || miss != 0;
             // (the tile before is widened everywhere: its factors go)
             named_barrier_sync(1, 128);
@@ -498,17 +524,17 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
                 uint32_t f = f16_pow2x2(__byte_perm(w, 0u, h == 0 ? 0x4140 : 0x4342), c_tile + 127);
                 // behind the last key (or on a page that is not there) anything may stand: values count as zero
                 if (x == 1 && cut && (ct >= there || ((miss >> (ct >> 4)) & 1u))) f = 0u;
-                uint16_t* at = &factors[x][2 * h * kWdTile + (ct & 7) * 16 + (ct >> 3)];
+                uint16_t* at = &factors[READY ? 0 : x][2 * h * kWdTile + (ct & 7) * 16 + (ct >> 3)];
                 at[0] = static_cast<uint16_t>(f);
                 at[kWdTile] = static_cast<uint16_t>(f >> 16);
               }
             }
-            if (ct == 0) exponents[slot] = make_int2(cs[0], cs[1]);
+            if (ct == 0) { info[slot].ck = cs[0]; info[slot].cv = cs[1]; }
             named_barrier_sync(1, 128);
           }
           const uint8_t* codes = base + Cfg::kCodeAt + st * Cfg::kCodeBytes + code_at;
           uint8_t* dst = base + Cfg::kF16At + st * Cfg::kF16Bytes + f16_at;
-          const uint4 fs = *reinterpret_cast<const uint4*>(&factors[v][b * kWdTile + (r0 & 7) * 16 + half * 8]);
+          const uint4 fs = *reinterpret_cast<const uint4*>(&factors[READY ? 0 : v][b * kWdTile + (r0 & 7) * 16 + half * 8]);
           const uint32_t fw[4] = {fs.x, fs.y, fs.z, fs.w};
           auto widen = [&](auto check) {
 #pragma unroll
@@ -543,8 +569,37 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
       }
     }
   } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kWdRegsIssue));
-    if (warp == 12) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Shape::kRegsIssue));
+    if (READY && warp == Shape::kIssueWarp) {
+      // ---------------------------------------------------------------- widened tiles, 32 KB (16 KB) a copy
+      uint32_t n_step = 0;
+      int turn = 0;
+      bool ok = true;
+      for (int k = 0; ok && item_at(k, &it); ++k) {
+        const int64_t line = (static_cast<int64_t>(it.seq) * p.kv_heads + it.head) * wp.max_tiles;
+        for (int t = it.tile0; ok && t < it.tile1; ++t, ++turn) {
+#pragma unroll
+          for (int v = 0; v < 2; ++v, ++n_step) {
+            const uint32_t st = n_step % kStages, phase = (n_step / kStages) & 1u;
+            ok = __all_sync(0xFFFFFFFFu, mbar_wait_short(smem_u32(&f16_empty[st]), phase ^ 1u, &abort_flag));
+            if (!ok) break;
+            if (lane == 0) {
+              const uint32_t bar = smem_u32(&f16_full[st]);
+              mbar_arrive_expect_tx(bar, Cfg::kF16Bytes + (v == 0 ? static_cast<int>(sizeof(AttnTileInfo)) : 0));
+              if (v == 0) bulk_g2s(smem_u32(&info[turn % Cfg::kScaleSlots]), wp.info + line + t, sizeof(AttnTileInfo), bar);
+              bulk_g2s(smem_u32(base + Cfg::kF16At + st * Cfg::kF16Bytes), wp.tiles + ((line + t) * 2 + v) * Cfg::kF16Bytes, Cfg::kF16Bytes, bar);
+            }
+            __syncwarp();
+          }
+        }
+      }
+      if (!ok) {   // given up: copies already in flight land before the CTA leaves
+        for (uint32_t i = n_step > kStages ? n_step - kStages : 0; i < n_step; ++i) {
+          const uint64_t t0 = global_timer_ns();
+          while (!mbar_try_wait(smem_u32(&f16_full[i % kStages]), (i / kStages) & 1u) && global_timer_ns() - t0 < 100000000ull) {}
+        }
+      }
+    } else if (!READY && warp == Shape::kIssueWarp) {
       // ---------------------------------------------------------------- codes and scales by TMA
       const int box = min(1 << p.page_shift, 32), boxes = kWdTile / box;   // rows of a copy; copies of a tile
       uint32_t n_step = 0;
@@ -568,7 +623,7 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
           const int row = ((page * p.kv_heads + it.head) << p.page_shift) + (tok & ((1 << p.page_shift) - 1));   // below 2^31
 #pragma unroll
           for (int v = 0; v < 2; ++v, ++n_step) {
-            const uint32_t st = n_step % kWdStages, phase = (n_step / kWdStages) & 1u;
+            const uint32_t st = n_step % kStages, phase = (n_step / kStages) & 1u;
             ok = __all_sync(0xFFFFFFFFu, mbar_wait_short(smem_u32(&code_empty[st]), phase ^ 1u, &abort_flag));
             if (!ok) break;
             const uint32_t bar = smem_u32(&code_full[st]);
@@ -577,7 +632,7 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
                 uint32_t miss = 0;
                 for (int i = 0; i < boxes; ++i)
                   if ((lost >> i) & 1u) miss |= (box == 32 ? 3u : 1u) << (i * (box / 16));
-                missing[slot] = miss;
+                info[slot].missing = miss;
                 if (miss != 0) atomicOr(&g_device_error, kErrorIndex);
               }
               mbar_arrive_expect_tx(bar, n_have * box * (D + (v == 0 ? 2 * BL : 0)));
@@ -599,12 +654,12 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
         }
       }
       if (!ok) {   // given up: copies already in flight land before the CTA leaves
-        for (uint32_t i = n_step > kWdStages ? n_step - kWdStages : 0; i < n_step; ++i) {
+        for (uint32_t i = n_step > kStages ? n_step - kStages : 0; i < n_step; ++i) {
           const uint64_t t0 = global_timer_ns();
-          while (!mbar_try_wait(smem_u32(&code_full[i % kWdStages]), (i / kWdStages) & 1u) && global_timer_ns() - t0 < 100000000ull) {}
+          while (!mbar_try_wait(smem_u32(&code_full[i % kStages]), (i / kStages) & 1u) && global_timer_ns() - t0 < 100000000ull) {}
         }
       }
-    } else if (warp == 13) {
+    } else if (warp == Shape::kIssueWarp + 1) {
       // ---------------------------------------------------------------- MMAs
       constexpr uint32_t idesc_s = f16_idesc_f16(128, kWdTile, false), idesc_o = f16_idesc_f16(128, D, true);
       const uint64_t q_desc = make_smem_desc(smem_u32(base), 16, 1024, 2);                              // K-major, 128-byte swizzle
@@ -635,17 +690,17 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
         for (int g = 0; g < groups && wait(&q_ready[g], q_phase[g]); ++g) q_phase[g] ^= 1u;
         if (!ok) break;
         // step of tile j: K n_step + 2 j, V n_step + 2 j + 1
-        if (!wait(&f16_full[n_step % kWdStages], (n_step / kWdStages) & 1u)) break;
+        if (!wait(&f16_full[n_step % kStages], (n_step / kStages) & 1u)) break;
         tc_fence_after_sync();
-        for (int g = 0; g < groups; ++g) scores(g, n_step % kWdStages);
-        if (elect_one()) tc_commit(smem_u32(&f16_empty[n_step % kWdStages]));
+        for (int g = 0; g < groups; ++g) scores(g, n_step % kStages);
+        if (elect_one()) tc_commit(smem_u32(&f16_empty[n_step % kStages]));
         __syncwarp();
         for (int j = 0; ok && j < n; ++j) {
-          const uint32_t vn = n_step + 2 * j + 1, kn = vn + 1, vst = vn % kWdStages, kst = kn % kWdStages;
+          const uint32_t vn = n_step + 2 * j + 1, kn = vn + 1, vst = vn % kStages, kst = kn % kStages;
           for (int g = 0; g < groups; ++g) {
             if (!wait(&p_ready[g], p_phase[g])) break;
             p_phase[g] ^= 1u;
-            if (g == 0 && !wait(&f16_full[vst], (vn / kWdStages) & 1u)) break;
+            if (g == 0 && !wait(&f16_full[vst], (vn / kStages) & 1u)) break;
             tc_fence_after_sync();
             if (elect_one()) {
               const uint64_t v = v_desc + static_cast<uint32_t>((vst * Cfg::kF16Bytes) >> 4);
@@ -657,7 +712,7 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
             }
             __syncwarp();
             if (j + 1 < n) {
-              if (g == 0 && !wait(&f16_full[kst], (kn / kWdStages) & 1u)) break;
+              if (g == 0 && !wait(&f16_full[kst], (kn / kStages) & 1u)) break;
               tc_fence_after_sync();
               scores(g, kst);
               if (g == groups - 1) {
@@ -678,9 +733,92 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
   }
   tc_fence_before_sync();
   __syncthreads();
-  if (warp == 13) {
+  if (warp == Shape::kIssueWarp + 1) {
     tc_fence_after_sync();
     tmem_dealloc(tmem_base_smem, 512);
+  }
+}
+
+// K and V of the sequences that attention_kv_wide_kernel takes, widened once for all its units: CTA (tile, head, sequence)
+// writes the two f16 tiles as they will stand in shared memory, and their AttnTileInfo.
+template <int D>
+__global__ void __launch_bounds__(128) attention_widen_kernel(const __grid_constant__ AttnWideParams wp, const uint8_t* __restrict__ k_codes,
+                                                              const uint8_t* __restrict__ v_codes) {
+  using Cfg = AttnWideCfg<D, true>;
+  constexpr int BL = Cfg::kBlocks, kChunks = D / 16;   // 16-code chunks of a row
+  const AttnParams& p = wp.a;
+  __shared__ int rows[kWdTile];                    // a token's row of the pool, -1: none
+  __shared__ uint16_t factors[2][kWdTile * BL];
+  __shared__ uint32_t tops[2][4], lost[4];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int t = blockIdx.x, head = blockIdx.y, seq = blockIdx.z;
+  grid_launch_dependents();
+  grid_dependency_wait();
+  const AttnSeq sq = attn_seq(p, seq);
+  if (sq.nq * p.group < wp.least_rows || t * kWdTile >= sq.len) return;
+  const int tok = t * kWdTile + tid;
+  int row = -1;
+  bool miss = false;
+  if (tok < sq.len) {
+    const int page = p.page_table[static_cast<int64_t>(seq) * p.ld_pages + (tok >> p.page_shift)];
+    miss = static_cast<uint32_t>(page) >= static_cast<uint32_t>(p.pages);
+    if (!miss) row = ((page * p.kv_heads + head) << p.page_shift) + (tok & ((1 << p.page_shift) - 1));   // below 2^31
+  }
+  rows[tid] = row;
+  uint32_t w[2] = {0u, 0u};   // the token's scale bytes
+  if (row >= 0) {
+    if (BL == 4) {
+      w[0] = *reinterpret_cast<const uint32_t*>(p.k_scales + static_cast<int64_t>(row) * 4);
+      w[1] = *reinterpret_cast<const uint32_t*>(p.v_scales + static_cast<int64_t>(row) * 4);
+    } else {
+      w[0] = *reinterpret_cast<const uint16_t*>(p.k_scales + static_cast<int64_t>(row) * 2);
+      w[1] = *reinterpret_cast<const uint16_t*>(p.v_scales + static_cast<int64_t>(row) * 2);
+    }
+  }
+  const uint32_t gone = __ballot_sync(0xFFFFFFFFu, miss);
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+    uint32_t top = __vmaxu4(w[x], w[x] >> 16);
+    top = __reduce_max_sync(0xFFFFFFFFu, max(top & 255u, (top >> 8) & 255u));
+    if (lane == 0) tops[x][warp] = top;
+  }
+  if (lane == 0) lost[warp] = (gone & 0xFFFFu ? 1u : 0u) | (gone >> 16 ? 2u : 0u);
+  __syncthreads();
+  int c[2];
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+    const uint32_t top = max(max(tops[x][0], tops[x][1]), max(tops[x][2], tops[x][3]));
+    c[x] = max(static_cast<int>(top) - 127 - 7, x == 0 ? -100 : kAtMinScale);
+#pragma unroll
+    for (int h = 0; h < BL / 2; ++h) {
+      const uint32_t f = f16_pow2x2(__byte_perm(w[x], 0u, h == 0 ? 0x4140 : 0x4342), c[x] + 127);
+      *reinterpret_cast<uint32_t*>(&factors[x][tid * BL + 2 * h]) = row >= 0 ? f : 0u;
+    }
+  }
+  const int64_t at = (static_cast<int64_t>(seq) * p.kv_heads + head) * wp.max_tiles + t;
+  if (tid == 0) {
+    const uint32_t all = lost[0] | lost[1] << 2 | lost[2] << 4 | lost[3] << 6;
+    wp.info[at] = AttnTileInfo{c[0], c[1], all, 0};
+    if (all != 0) atomicOr(&g_device_error, kErrorIndex);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int v = 0; v < 2; ++v) {
+    const uint8_t* codes = v == 0 ? k_codes : v_codes;
+    uint8_t* dst = wp.tiles + (at * 2 + v) * Cfg::kF16Bytes;
+#pragma unroll 4
+    for (int i = 0; i < kChunks; ++i) {
+      const int n = i * 128 + tid, r = n / kChunks, ch = n % kChunks;
+      uint4 q = make_uint4(0u, 0u, 0u, 0u);   // a token that is not there is zero, whatever stands on its page
+      if (rows[r] >= 0) q = *reinterpret_cast<const uint4*>(codes + static_cast<int64_t>(rows[r]) * D + ch * 16);
+      const uint32_t f = factors[v][r * BL + (ch >> 1)] * 0x10001u;
+      uint8_t* line = dst + (ch >> 2) * Cfg::kHalfTile + r * 128;
+      const int p0 = (ch & 3) * 2;
+      *reinterpret_cast<uint4*>(line + ((p0 ^ (r & 7)) << 4)) = make_uint4(hmul2(e4m3x2_to_f16x2(q.x), f), hmul2(e4m3x2_to_f16x2_high(q.x), f),
+                                                                         hmul2(e4m3x2_to_f16x2(q.y), f), hmul2(e4m3x2_to_f16x2_high(q.y), f));
+      *reinterpret_cast<uint4*>(line + (((p0 + 1) ^ (r & 7)) << 4)) = make_uint4(hmul2(e4m3x2_to_f16x2(q.z), f), hmul2(e4m3x2_to_f16x2_high(q.z), f),
+                                                                               hmul2(e4m3x2_to_f16x2(q.w), f), hmul2(e4m3x2_to_f16x2_high(q.w), f));
+    }
   }
 }
 

@@ -199,8 +199,10 @@ batq_status device_setup(int* device_out, const DeviceInfo** info_out) {
     e = e ? e : set_smem(attention_kv_kernel<128, 2>, AttnCfg<128, 2>::kSmemBytes);
     e = e ? e : set_smem(attention_kv_kernel<64, 1>, AttnCfg<64, 1>::kSmemBytes);
     e = e ? e : set_smem(attention_kv_kernel<64, 2>, AttnCfg<64, 2>::kSmemBytes);
-    e = e ? e : set_smem(attention_kv_wide_kernel<128>, AttnWideCfg<128>::kSmemBytes);
-    e = e ? e : set_smem(attention_kv_wide_kernel<64>, AttnWideCfg<64>::kSmemBytes);
+    e = e ? e : set_smem(attention_kv_wide_kernel<128, false>, AttnWideCfg<128, false>::kSmemBytes);
+    e = e ? e : set_smem(attention_kv_wide_kernel<128, true>, AttnWideCfg<128, true>::kSmemBytes);
+    e = e ? e : set_smem(attention_kv_wide_kernel<64, false>, AttnWideCfg<64, false>::kSmemBytes);
+    e = e ? e : set_smem(attention_kv_wide_kernel<64, true>, AttnWideCfg<64, true>::kSmemBytes);
     if (e != cudaSuccess) { cudaGetLastError(); return BATQ_ERR_CUDA; }
     if (g_encode_tiled == nullptr) {
       void* fn = nullptr;
@@ -1712,6 +1714,8 @@ cudaError_t launch_append(int gc, int grid, const KvAppendParams& p, cudaStream_
 // attention_kv_kernel, the others to attention_kv_wide_kernel; a call of one sequence that may have more makes one
 // launch only.
 constexpr int kNarrowRows = 32;
+constexpr int kReadyUnits = 3;
+constexpr size_t kReadyBytes = size_t(512) << 20;
 struct AttnPlan {
   bool narrow, wide;
   int nt, grid;                         // narrow: rows of a unit / 8, CTAs
@@ -1719,6 +1723,9 @@ struct AttnPlan {
   int wide_grid, wide_items, wide_units;
   size_t part_ml, join;                 // offsets of the narrow part's workspace; the partial sums are its start
   size_t wide_o, wide_ml, wide_join, wide_plan;
+  bool ready;                           // K and V are widened into the workspace first
+  int max_tiles;
+  size_t ready_tiles, ready_info;
   size_t bytes;
 };
 bool plan_attention(const batq_kv_cache* c, int32_t q_heads, int32_t seqs, int32_t max_q, int32_t max_kv, AttnPlan* a) {
@@ -1755,6 +1762,18 @@ bool plan_attention(const batq_kv_cache* c, int32_t q_heads, int32_t seqs, int32
     a->wide_join = a->wide_ml + round_up(rows * sizeof(float2), 256);
     a->wide_plan = a->wide_join + round_up((a->wide_units + 1) * sizeof(AttnJoin), 256);
     a->bytes = a->wide_plan + 256;
+    // Every unit of a sequence and head reads all the tokens in front of its last row: widening them once is worth a
+    // kernel of its own from a few units on, as long as the f16 copy stays of a size.
+    const int64_t per_head = (most + kWdRows - 1) / kWdRows;
+    const size_t tile_bytes = 2 * static_cast<size_t>(kWdTile) * c->head_dim * 2;
+    const size_t copy = static_cast<size_t>(batch) * c->kv_heads * std::max<int64_t>(1, tiles) * tile_bytes;
+    a->max_tiles = static_cast<int>(std::max<int64_t>(1, tiles));
+    a->ready = per_head >= kReadyUnits && copy <= kReadyBytes && a->max_tiles <= 65535 * 16 && batch <= 65535 && c->kv_heads <= 65535;
+    if (a->ready) {
+      a->ready_tiles = round_up(a->bytes, 1024);
+      a->ready_info = a->ready_tiles + copy;
+      a->bytes = a->ready_info + round_up(copy / tile_bytes * sizeof(AttnTileInfo), 256);
+    }
   }
   return true;
 }
@@ -1783,10 +1802,15 @@ cudaError_t launch_attention(const batq_kv_cache* c, const AttnPlan& a, const At
   return e != cudaSuccess || !a.joins ? e : launch_dependent(attention_join_kernel<D, NT>, grid, NT * 256, 0, stream, p);
 }
 
-template <int D>
+template <int D, bool READY>
 cudaError_t launch_attention_wide(const batq_kv_cache* c, const AttnPlan& a, const AttnWideParams& p, cudaStream_t stream) {
-  const cudaError_t e = launch_dependent(attention_kv_wide_kernel<D>, dim3(static_cast<unsigned>(a.wide_grid)), kWdThreads, AttnWideCfg<D>::kSmemBytes,
-                                         stream, c->tmap_k, c->tmap_v, p);
+  cudaError_t e = cudaSuccess;
+  if (READY)
+    e = launch_dependent(attention_widen_kernel<D>, dim3(static_cast<unsigned>(a.max_tiles), static_cast<unsigned>(c->kv_heads), static_cast<unsigned>(p.a.seqs)),
+                         128, 0, stream, p, static_cast<const uint8_t*>(c->k_codes), static_cast<const uint8_t*>(c->v_codes));
+  if (e != cudaSuccess) return e;
+  e = launch_dependent(attention_kv_wide_kernel<D, READY>, dim3(static_cast<unsigned>(a.wide_grid)), AttnWideShape<D, READY>::kThreads,
+                       AttnWideCfg<D, READY>::kSmemBytes, stream, c->tmap_k, c->tmap_v, p);
   if (e != cudaSuccess || a.wide_units == 0) return e;
   return launch_dependent(attention_wide_join_kernel<D>, dim3(static_cast<unsigned>(a.wide_units), kWdRows / 8), 256, 0, stream, p);
 }
@@ -2836,7 +2860,11 @@ batq_status batq_attention_kv_mxfp8(const batq_kv_cache* c, const void* q_bf16, 
       wp.plan = reinterpret_cast<AttnWidePlan*>(ws + a.wide_plan);
       wp.least_rows = a.narrow ? kNarrowRows + 1 : 1;
       wp.max_items = a.wide_items;
-      e = c->head_dim == 128 ? launch_attention_wide<128>(c, a, wp, cs) : launch_attention_wide<64>(c, a, wp, cs);
+      wp.max_tiles = a.max_tiles;
+      wp.tiles = a.ready ? ws + a.ready_tiles : nullptr;
+      wp.info = a.ready ? reinterpret_cast<AttnTileInfo*>(ws + a.ready_info) : nullptr;
+      e = c->head_dim == 128 ? (a.ready ? launch_attention_wide<128, true>(c, a, wp, cs) : launch_attention_wide<128, false>(c, a, wp, cs))
+                             : (a.ready ? launch_attention_wide<64, true>(c, a, wp, cs) : launch_attention_wide<64, false>(c, a, wp, cs));
     }
     if (e != cudaSuccess) { cudaGetLastError(); return BATQ_ERR_CUDA; }
   }
