@@ -239,8 +239,8 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
     const int64_t at = static_cast<int64_t>(k) * grid + ((k & 1) ? grid - 1 - b : b);
     if (at >= items) return false;
     const int i = static_cast<int>(at);
-    it->unit = i / splits;
-    it->split = i % splits;
+    it->unit = splits == 1 ? i : i / splits;
+    it->split = i - it->unit * splits;
     int lo = 0, hi = p.seqs - 1;   // the last sequence that starts at or before the unit
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
@@ -250,13 +250,14 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
     it->seq = lo;
     it->sq = attn_seq(p, lo);
     const int rows = it->sq.nq * p.group, row_tiles = (rows + kWdRows - 1) / kWdRows, local = it->unit - first[lo];
-    it->head = local % p.kv_heads;
-    it->row0 = (row_tiles - 1 - local / p.kv_heads) * kWdRows;
+    const int up = local / p.kv_heads;
+    it->head = local - up * p.kv_heads;
+    it->row0 = (row_tiles - 1 - up) * kWdRows;
     it->n_rows = min(kWdRows, rows - it->row0);
     it->end = attn_visible(p, it->sq, (it->row0 + it->n_rows - 1) / p.group);
-    const int64_t tiles = (it->end + kWdTile - 1) / kWdTile;
-    it->tile0 = static_cast<int>(tiles * it->split / splits);
-    it->tile1 = static_cast<int>(tiles * (it->split + 1) / splits);
+    const int tiles = (it->end + kWdTile - 1) / kWdTile;   // times the parts of a unit: below 2^31
+    it->tile0 = splits == 1 ? 0 : tiles * it->split / splits;
+    it->tile1 = splits == 1 ? tiles : tiles * (it->split + 1) / splits;
     return true;
   };
 
@@ -697,10 +698,12 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
         __syncwarp();
         for (int j = 0; ok && j < n; ++j) {
           const uint32_t vn = n_step + 2 * j + 1, kn = vn + 1, vst = vn % kStages, kst = kn % kStages;
+          // These are here long before the weights are, and asking for them takes some 400 cycles: not between products.
+          if (!wait(&f16_full[vst], (vn / kStages) & 1u)) break;
+          if (j + 1 < n && !wait(&f16_full[kst], (kn / kStages) & 1u)) break;
           for (int g = 0; g < groups; ++g) {
             if (!wait(&p_ready[g], p_phase[g])) break;
             p_phase[g] ^= 1u;
-            if (g == 0 && !wait(&f16_full[vst], (vn / kStages) & 1u)) break;
             tc_fence_after_sync();
             if (elect_one()) {
               const uint64_t v = v_desc + static_cast<uint32_t>((vst * Cfg::kF16Bytes) >> 4);
@@ -712,8 +715,6 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
             }
             __syncwarp();
             if (j + 1 < n) {
-              if (g == 0 && !wait(&f16_full[kst], (kn / kStages) & 1u)) break;
-              tc_fence_after_sync();
               scores(g, kst);
               if (g == groups - 1) {
                 if (elect_one()) tc_commit(smem_u32(&f16_empty[kst]));
