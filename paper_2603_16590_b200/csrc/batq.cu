@@ -199,6 +199,8 @@ batq_status device_setup(int* device_out, const DeviceInfo** info_out) {
     e = e ? e : set_smem(attention_kv_kernel<128, 2>, AttnCfg<128, 2>::kSmemBytes);
     e = e ? e : set_smem(attention_kv_kernel<64, 1>, AttnCfg<64, 1>::kSmemBytes);
     e = e ? e : set_smem(attention_kv_kernel<64, 2>, AttnCfg<64, 2>::kSmemBytes);
+    e = e ? e : set_smem(attention_kv_kernel<128, 3>, AttnCfg<128, 3>::kSmemBytes);
+    e = e ? e : set_smem(attention_kv_kernel<64, 3>, AttnCfg<64, 3>::kSmemBytes);
     e = e ? e : set_smem(attention_kv_wide_kernel<128, false>, AttnWideCfg<128, false>::kSmemBytes);
     e = e ? e : set_smem(attention_kv_wide_kernel<128, true>, AttnWideCfg<128, true>::kSmemBytes);
     e = e ? e : set_smem(attention_kv_wide_kernel<64, false>, AttnWideCfg<64, false>::kSmemBytes);
@@ -1735,12 +1737,11 @@ bool plan_attention(const batq_kv_cache* c, int32_t q_heads, int32_t seqs, int32
   a->narrow = !a->wide || seqs > 1;
   if (a->narrow) {
     const int64_t rows = std::min<int64_t>(most, kNarrowRows);
-    a->nt = rows <= 8 ? 1 : 2;
+    a->nt = rows <= 8 ? 1 : rows <= 16 || rows > 24 ? 2 : 3;   // as few units as can be; more rows than 24 of one do not fit the registers
     const int64_t units = (rows + 8 * a->nt - 1) / (8 * a->nt) * c->kv_heads * batch;
     const int64_t tiles = std::max<int64_t>(1, (static_cast<int64_t>(max_kv) + kAtTile - 1) / kAtTile);
     if (units > INT_MAX || units * (tiles + kAtUnitCost) > INT_MAX) return false;   // the kernel counts tiles in 32 bits
-    const int per_sm = c->head_dim == 128 ? (a->nt == 1 ? AttnCfg<128, 1>::kCtasPerSm : AttnCfg<128, 2>::kCtasPerSm)
-                                          : (a->nt == 1 ? AttnCfg<64, 1>::kCtasPerSm : AttnCfg<64, 2>::kCtasPerSm);
+    const int per_sm = a->nt == 1 ? AttnCfg<128, 1>::kCtasPerSm : AttnCfg<128, 2>::kCtasPerSm;
     a->grid = static_cast<int>(std::min<int64_t>(static_cast<int64_t>(per_sm) * c->sm_count, units * tiles));
     a->joins = tiles > kAtSnap && a->grid > 1;
     const size_t parts = static_cast<size_t>(a->grid) * 2 * 8 * a->nt;
@@ -2849,8 +2850,10 @@ batq_status batq_attention_kv_mxfp8(const batq_kv_cache* c, const void* q_bf16, 
       p.part_o = a.joins ? reinterpret_cast<float*>(ws) : nullptr;
       p.part_ml = a.joins ? reinterpret_cast<float2*>(ws + a.part_ml) : nullptr;
       p.join = a.joins ? reinterpret_cast<AttnJoin*>(ws + a.join) : nullptr;
-      e = c->head_dim == 128 ? (a.nt == 1 ? launch_attention<128, 1>(c, a, p, cs) : launch_attention<128, 2>(c, a, p, cs))
-                             : (a.nt == 1 ? launch_attention<64, 1>(c, a, p, cs) : launch_attention<64, 2>(c, a, p, cs));
+      if (c->head_dim == 128)
+        e = a.nt == 1 ? launch_attention<128, 1>(c, a, p, cs) : a.nt == 2 ? launch_attention<128, 2>(c, a, p, cs) : launch_attention<128, 3>(c, a, p, cs);
+      else
+        e = a.nt == 1 ? launch_attention<64, 1>(c, a, p, cs) : a.nt == 2 ? launch_attention<64, 2>(c, a, p, cs) : launch_attention<64, 3>(c, a, p, cs);
     }
     if (e == cudaSuccess && a.wide) {
       wp.a = p;
