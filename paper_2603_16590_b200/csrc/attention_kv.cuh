@@ -37,7 +37,7 @@ constexpr int kAtTile = 32;       // tokens a warp takes at a time
 constexpr int kAtStages = 2;       // x 8.4 KB x 4 warps: three CTAs on an SM
 constexpr int kAtSnap = 8;        // units of up to this many tiles are not divided
 constexpr int kAtMaxSeqs = 512;   // sequences of one launch
-constexpr int kAtUnitCost = 8;    // what a unit costs besides its tiles, in tiles (4 us: look-ups, first loads, the merge)
+constexpr int kAtUnitCost = 12;   // what a unit costs besides its tiles, in tiles (look-ups, first loads, the merge; 6: 115 us, 8: 113, 12: 110 for 128 ragged sequences)
 constexpr float kAtSlack = 8.0f;  // how far (log2) a score may stand above the reference: weights up to 2^8 in f16
 constexpr float kAtNone = -1e30f; // the reference of a row that has seen no key
 constexpr int kAtMinScale = -32;  // least c: an all-zero tile must not push the softmax sum's terms out of fp32

@@ -176,11 +176,11 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
       tma_prefetch_desc(&tmap_v);
     }
   }
-  if (warp == Shape::kIssueWarp + 1) {
+  grid_dependency_wait();   // q, the lengths and the cache may come from the grid in front
+  if (warp == Shape::kIssueWarp + 1) {   // not before: the grid in front may still want tensor memory of this SM
     tmem_alloc(smem_u32(&tmem_base_smem), 512);
     tmem_relinquish();
   }
-  grid_dependency_wait();   // q, the lengths and the cache may come from the grid in front
 
   // units of each sequence, of all, and the most tiles of one
   int units, splits;

@@ -153,6 +153,25 @@ def test_bounds_may_be_larger_than_the_batch(batq, rows):
     b.check(*b.run(batq, max_q=300, max_kv=20000))
 
 
+@pytest.mark.parametrize("max_kv,ready", [(700, True), (200000, False)])
+def test_keys_widened_once_or_by_every_unit(batq, max_kv, ready):
+    """Prompts of several units: from an f16 copy in the workspace, or where that would be too large (200000 keys for
+    each of three sequences) from the codes; both against the definition."""
+    b = Batch(batq, 32, 8, 128, 64, [150, 1, 77], [700, 64, 77], seed=20)
+    n = batq.batq_attention_kv_mxfp8_workspace_bytes(b.cache, 32, 228, 3, 150, max_kv)
+    copy = 3 * 8 * -(-max_kv // 128) * 65536
+    assert (n >= copy) == ready
+    b.check(*b.run(batq, max_kv=max_kv))
+
+
+@pytest.mark.parametrize("rows", [1, 5, 70])
+def test_no_keys_at_all(batq, rows):
+    b = Batch(batq, 8, 2, 64, 16, [rows, rows], [0, 0], seed=21)
+    for max_kv in (0, 1, 500):
+        out, lse = b.run(batq, max_kv=max_kv)
+        assert (out == 0).all() and torch.isinf(lse).all() and (lse < 0).all()
+
+
 def test_lengths_beyond_the_bounds_are_not_looked_at(batq):
     b = Batch(batq, 8, 2, 128, 32, [1, 1], [100, 90], seed=7)
     got, _ = b.run(batq, max_kv=64)
