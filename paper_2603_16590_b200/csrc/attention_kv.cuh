@@ -7,7 +7,7 @@
 // tiles (32 tokens) of all units of the batch stand in one line, cut into ranges of equal cost, one for each CTA that the device
 // holds at once: a ragged batch, one long sequence and many short ones all keep every SM at work to the end.  (A CTA per
 // fixed piece of a sequence instead: 33 against 25 us for 16 sequences of up to 4001 keys, 137 against 58 for one of
-// 131072, 124 against 107 for 128 of up to 8192.)  A cut never falls into a unit of up to kAtSnap tiles; what a cut
+// 131072, 124 against 110 for 128 of up to 8192.)  A cut never falls into a unit of up to kAtSnap tiles; what a cut
 // divides is joined from the workspace, in the order of the tokens, by attention_join_kernel.
 //
 // Within a range a CTA's four warps take every fourth tile and are independent of one another until the unit ends: each

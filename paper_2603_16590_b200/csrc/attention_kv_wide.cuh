@@ -10,12 +10,20 @@
 //   warps 0-7      softmax: a thread owns a row.  While one M tile's warps are in their exponentials, the tensor cores are
 //                  at the other's products.  The reference follows the maximum only beyond 2^8 (as in attention_kv.cuh),
 //                  so O is hardly ever read back before the end.
-//   warps 8-11     widen the codes: K 2^(ek - ck) and V 2^(ev - cv) in f16, ck and cv one integer per 128 tokens, into
-//                  128-byte-swizzled tiles (K: K-major B operand; V: MN-major B operand, the same bytes).  They are widened
-//                  once per 256 rows; the block-scaled kinds would take the codes as they are, but want q and P in 8 bits,
-//                  and V's scales along the wrong axis.
-//   warp 12        TMA: codes and scales, page by page, three tiles ahead
-//   warp 13        issues the MMAs
+//   the others     one warp brings tiles, one issues the MMAs, and without READY four widen the codes: K 2^(ek - ck) and
+//                  V 2^(ev - cv) in f16, ck and cv one integer per 128 tokens, into 128-byte-swizzled tiles (K: K-major B
+//                  operand; V: MN-major B operand, the same bytes).  The block-scaled kinds would take the codes as they
+//                  are, but want q and P in 8 bits, and V's scales along the wrong axis.
+//
+// What bounds it is instruction issue beside the exponentials: on each of an SM's four schedulers two softmax warps (some
+// 450 instructions a tile each; 128 exponentials of 8 cycles) take 2260 cycles a tile by themselves, and the four widening
+// warps, 250 instructions a tile, double that (measured in isolation).  So where a sequence and head has three units or
+// more, attention_widen_kernel writes the f16 tiles to the workspace once and this kernel copies them (READY): a prompt
+// of 8192 tokens, 28 / 4 heads, takes 490 us (0.98 PFLOP/s, 0.6 of what a large bf16 product reaches) against 742, one of
+// 2048, 32 / 8 heads, 71 against 82.  A tile pair then takes some 3900 cycles: 2200 of softmax, 1100 of products, the rest
+// waits and issue.  An item's end and the next one's start cost some 15000.
+// Tried without gain: sixteen softmax warps of 64 columns (registers: the scores have to be read twice; 10000 cycles a
+// tile), naps between two looks at a barrier, q of the next item brought early (1.7 % slower).
 //
 // Units go to the CTAs (one per SM) longest first, alternately up and down.  Where there are few, each is divided along
 // its tokens into as many parts as finish soonest; attention_wide_join_kernel adds the parts up in order.

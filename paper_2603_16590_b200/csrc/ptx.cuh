@@ -102,14 +102,11 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
 
 // The same for waits of a few hundred cycles that something else waits for in turn: no parking, whose wake-up
 // costs more than the wait.  The limits are looked at every 256 tries.
-template <int kNap = 0>   // nanoseconds between two tries: a warp that tries without rest takes issue slots from the others
 __device__ __forceinline__ bool mbar_wait_short(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
   uint64_t t0 = 0;
   for (;;) {
-    for (int i = 0; i < 256; ++i) {
+    for (int i = 0; i < 256; ++i)
       if (mbar_try_wait(bar, parity)) return true;
-      if (kNap > 0) __nanosleep(kNap);
-    }
     if (*abort_flag) return false;
     const uint64_t now = global_timer_ns();
     if (t0 == 0) t0 = now;
