@@ -356,10 +356,13 @@ batq_status batq_kv_append_mxfp8(const batq_kv_cache* c, const batq_transform* t
  *                them, or beyond ld_pages * page_size keys, is not looked at.
  *   lse          dev fp32 [tokens x q_heads] or NULL.
  *   workspace    dev, batq_attention_kv_mxfp8_workspace_bytes(...) bytes with the same sizes (may be 0), 256-byte
- *                aligned; contents need not be initialised; calls sharing it must be ordered on one stream.
- * The result of a row is the same whenever its call's sizes (seqs, max_q, max_kv, heads) are: nothing depends on the order in which
- * parts finish.  Finite q, keys and values; values within one block of 32 tokens that are more than 2^28 smaller
- * than its largest may be taken as 0.  seqs == 0 or tokens == 0 is a no-op.
+ *                aligned; contents need not be initialised; calls sharing it must be ordered on one stream.  A few MB
+ *                for decoding; with query rows for three or more units of 256 (rows x heads of a group) also an f16
+ *                copy of the keys and values, seqs * max_kv * kv_heads * head_dim * 4 bytes, where that is at most 512 MB.
+ * Repeated, a call gives the same bits: nothing depends on the order in which parts finish.  The last bits of a row may
+ * depend on the lengths of the other sequences, which move the places where long sequences are divided.  Finite q, keys
+ * and values; a value that is more than 2^28 smaller than the largest of the 128 tokens it stands with (tokens 128 i to
+ * 128 i + 127 of a sequence) is rounded to a multiple of 2^-40 of that.  seqs == 0 or tokens == 0 is a no-op.
  * Errors: NULL / SHAPE / ALIGN / UNSUPPORTED / WORKSPACE / CUDA. */
 size_t batq_attention_kv_mxfp8_workspace_bytes(const batq_kv_cache* c, int32_t q_heads, int64_t tokens, int32_t seqs,
                                                int32_t max_q, int32_t max_kv);
