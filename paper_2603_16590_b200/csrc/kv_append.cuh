@@ -291,13 +291,15 @@ __global__ void __launch_bounds__(kKvThreads, GC == 8 || GC == 0 ? 3 : 2) kv_app
       }
       continue;
     }
-    float mn = o[0], mx = o[0];
+    float mn = INFINITY, mx = -INFINITY;   // NaN counts as neither
 #pragma unroll
-    for (int i = 1; i < 32; ++i) {
+    for (int i = 0; i < 32; ++i) {
       mn = fminf(mn, o[i]);
       mx = fmaxf(mx, o[i]);
     }
-    if (r.clip_lo != nullptr) {
+    // Without a clip the ratios are 1 and the bounds the block's own: they take a NaN to a number.  No NaN code is ever
+    // stored: in an attention it would reach rows that do not see its token, as 0 times NaN.
+    {
       const float lo = clip_lo * mn, hi = clip_hi * mx;
 #pragma unroll
       for (int i = 0; i < 32; ++i) o[i] = fminf(fmaxf(o[i], lo), hi);

@@ -510,6 +510,46 @@ def test_append_is_the_quantiser_where_nothing_is_rotated(batq):
     assert (a.pool[1][at, :, off].view(-1, 4) != scales).double().mean() <= 1e-5
 
 
+@pytest.mark.parametrize("transform,clip", [(False, False), (True, False), (True, True)])
+def test_append_stores_no_nan(batq, transform, clip):
+    """A NaN (one element, a whole block) or an infinity: finite codes there, the other tokens as without it, and an
+    attention whose rows that do not see the token are the same."""
+    a = Append(batq, 60, 8, 2, 64, 16, rot=64, transform=transform, clip=clip, seed=12)
+    a.run(batq)
+    clean = [x.clone() for x in a.pool]
+    x = a.x.cuda().clone()
+    x[40, 8 * 64 + 3] = math.nan              # a key
+    x[40, 10 * 64:10 * 64 + 32] = math.nan    # a block of values
+    x[40, 11 * 64 + 40] = math.nan
+    x[50, 8 * 64 + 70] = math.inf
+    x[50, 9 * 64 + 1] = -math.inf
+    a.run(batq, x=x)
+    others = [i for i in range(60) if i not in (40, 50)]
+    at, off = (a.slots // 16).cuda(), (a.slots % 16).cuda()
+    for before, now in zip(clean, a.pool):
+        assert torch.equal(before[at, :, off][others], now[at, :, off][others])
+    for codes in (a.pool[0], a.pool[2]):
+        assert ((codes & 0x7F) != 0x7F).all()
+    table = torch.arange(a.pool[0].shape[0], dtype=torch.int32, device="cuda")[None].contiguous()
+    rows = torch.zeros(2, dtype=torch.int32, device="cuda")
+    # one sequence over the pool in slot order: the rows in front of the bad tokens' slots see none of them
+    first = int(min(a.slots[40], a.slots[50]))
+    n = table.shape[1] * 16
+    qs = torch.randn(n, 8 * 64, device="cuda", generator=torch.Generator("cuda").manual_seed(1)).bfloat16()
+    outs = []
+    for pool in (clean, a.pool):
+        cache = batq.batq_kv_cache_create(*[p.clone() for p in pool])
+        out = torch.zeros(n, 8 * 64, dtype=torch.bfloat16, device="cuda")
+        ws = batq.aligned_workspace(batq.batq_attention_kv_mxfp8_workspace_bytes(cache, 8, n, 1, n, n))
+        rows[1] = n
+        batq.batq_attention_kv_mxfp8(cache, qs, out, torch.tensor([n], dtype=torch.int32, device="cuda"), table, n, n, ws, q_starts=rows)
+        outs.append(out)
+    assert batq.batq_last_device_status() == 0
+    assert torch.isfinite(outs[1][:first].float()).all()
+    if int(a.slots[50]) > first + 128 or int(a.slots[50]) // 128 != first // 128:   # (an infinity's scale is felt within its tile)
+        assert torch.equal(outs[0][:first], outs[1][:first])
+
+
 def test_append_refuses(batq):
     a = Append(batq, 10, 8, 2, 128, 32, rot=128, seed=11)
     x = a.x.cuda()
