@@ -358,8 +358,8 @@ batq_status batq_kv_append_mxfp8(const batq_kv_cache* c, const batq_transform* t
  *   lse          dev fp32 [tokens x q_heads] or NULL.
  *   workspace    dev, batq_attention_kv_mxfp8_workspace_bytes(...) bytes with the same sizes (may be 0), 256-byte
  *                aligned; contents need not be initialised; calls sharing it must be ordered on one stream.  A few MB
- *                for decoding; with query rows for three or more units of 256 (rows x heads of a group) also an f16
- *                copy of the keys and values, seqs * max_kv * kv_heads * head_dim * 4 bytes, where that is at most 512 MB.
+ *                for decoding, up to 40 MB for prompts; where prompts pay for it, also an f16 copy of the keys and values,
+ *                seqs * max_kv * kv_heads * head_dim * 4 bytes, at most 512 MB.
  * Repeated, a call gives the same bits: nothing depends on the order in which parts finish.  The last bits of a row may
  * depend on the lengths of the other sequences, which move the places where long sequences are divided.  Finite q, keys
  * and values; a value that is more than 2^28 smaller than the largest of the 128 tokens it stands with (tokens 128 i to

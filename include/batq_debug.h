@@ -56,6 +56,9 @@ int32_t batq_debug_gemm_choice(int64_t s, int64_t m, int64_t n, int32_t sm_count
  * wide).  batq_debug_gemm_choice shows which one a call takes. */
 void batq_debug_force_gemm_kernel(int32_t which);
 
+/* Whether batq_attention_kv_mxfp8 widens keys and values into its workspace for prompts: 0 automatic, 1 never, 2 wherever the
+ * copy is small enough.  The workspace's size goes by it too. */
+void batq_debug_force_attention_copy(int32_t which);
 /* Which activation quantiser later calls use.  0 = automatic (up to 128 tokens the per-block ALU
  * kernel or, above 8192 (token, block) items, the thread-per-item ALU kernel, above 128 the
  * tensor-core dense-block kernel; the identity transform above 128 tokens and nothing else takes the

@@ -57,6 +57,7 @@ SIGNATURES = {
     "batq_debug_force_prefill_path": (None, [_I32]),
     "batq_debug_force_gemm_kernel": (None, [_I32]),
     "batq_debug_force_quantizer": (None, [_I32]),
+    "batq_debug_force_attention_copy": (None, [_I32]),
     "batq_linear_workspace_bytes": (_SZ, [_P, _I64]),
     "batq_linear_kernel_launches": (C.c_int32, [_P, _P, _I64]),
     "batq_debug_pair_schedule": (C.c_int32, [_I64, _I64, _I64, _I32, _I32, _P, _I32]),
@@ -363,6 +364,10 @@ def batq_debug_force_tile_width(bn: int):
 
 def batq_debug_force_gemm_kernel(which: int):
     load().batq_debug_force_gemm_kernel(which)
+
+
+def batq_debug_force_attention_copy(which: int):
+    load().batq_debug_force_attention_copy(which)
 
 
 def batq_debug_force_quantizer(which: int):

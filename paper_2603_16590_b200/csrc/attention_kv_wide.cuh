@@ -17,8 +17,8 @@
 //
 // What bounds it is instruction issue beside the exponentials: on each of an SM's four schedulers two softmax warps (some
 // 450 instructions a tile each; 128 exponentials of 8 cycles) take 2260 cycles a tile by themselves, and the four widening
-// warps, 250 instructions a tile, double that (measured in isolation).  So where a sequence and head has three units or
-// more, attention_widen_kernel writes the f16 tiles to the workspace once and this kernel copies them (READY): a prompt
+// warps, 250 instructions a tile, double that (measured in isolation).  So where a sequence and head has several units
+// and many tiles, attention_widen_kernel writes the f16 tiles to the workspace once and this kernel copies them (READY): a prompt
 // of 8192 tokens, 28 / 4 heads, takes 490 us (0.98 PFLOP/s, 0.6 of what a large bf16 product reaches) against 742, one of
 // 2048, 32 / 8 heads, 71 against 82.  A tile pair then takes some 3900 cycles: 2200 of softmax, 1100 of products, the rest
 // waits and issue.  An item's end and the next one's start cost some 15000.

@@ -1716,8 +1716,8 @@ cudaError_t launch_append(int gc, int grid, const KvAppendParams& p, cudaStream_
 // attention_kv_kernel, the others to attention_kv_wide_kernel; a call of one sequence that may have more makes one
 // launch only.
 constexpr int kNarrowRows = 32;
-constexpr int kReadyUnits = 3;
-constexpr size_t kReadyBytes = size_t(512) << 20;
+constexpr size_t kReadyBytes = size_t(512) << 20;   // most that the f16 copy of K and V may take
+std::atomic<int> g_force_attention_copy{0};         // tuning hook: 0 = automatic, 1 = never, 2 = wherever it fits
 struct AttnPlan {
   bool narrow, wide;
   int nt, grid;                         // narrow: rows of a unit / 8, CTAs
@@ -1730,7 +1730,7 @@ struct AttnPlan {
   size_t ready_tiles, ready_info;
   size_t bytes;
 };
-bool plan_attention(const batq_kv_cache* c, int32_t q_heads, int32_t seqs, int32_t max_q, int32_t max_kv, AttnPlan* a) {
+bool plan_attention(const batq_kv_cache* c, int32_t q_heads, int64_t tokens, int32_t seqs, int32_t max_q, int32_t max_kv, AttnPlan* a) {
   *a = AttnPlan{};
   const int64_t group = q_heads / c->kv_heads, most = max_q * group, batch = std::min<int32_t>(seqs, kAtMaxSeqs);
   a->wide = most > kNarrowRows;
@@ -1763,13 +1763,20 @@ bool plan_attention(const batq_kv_cache* c, int32_t q_heads, int32_t seqs, int32
     a->wide_join = a->wide_ml + round_up(rows * sizeof(float2), 256);
     a->wide_plan = a->wide_join + round_up((a->wide_units + 1) * sizeof(AttnJoin), 256);
     a->bytes = a->wide_plan + 256;
-    // Every unit of a sequence and head reads all the tokens in front of its last row: widening them once is worth a
-    // kernel of its own from a few units on, as long as the f16 copy stays of a size.
-    const int64_t per_head = (most + kWdRows - 1) / kWdRows;
+    // Every unit of a sequence and head reads all the tokens in front of its last row.  Widening them once saves each of
+    // its tiles some 1.1 us of an SM; it costs a tile of a head 0.02 us of the whole device and the call 7 us (measured on
+    // 1 and 8 sequences, 16 to 512 query rows behind 1024 and 8192 keys, 32 / 8 heads: e.g. 8 x 192 rows, 8192 keys 381
+    // us against 452 without, 8 x 512 654 / 937, 1 x 512 114 / 135; 1 x 256 88 / 80, 8 x 64 189 / 151, 1 x 512 behind 1024 45 / 38).
+    // The sequences that have many rows are taken to have max_q, the others one.
+    const double per_head = static_cast<double>((most + kWdRows - 1) / kWdRows);
+    const double wide_seqs = max_q <= 1 ? 1.0 : std::min<double>(static_cast<double>(batch), std::max(1.0, std::floor(static_cast<double>(tokens - seqs) / (max_q - 1) + 0.5)));
+    const double seen = std::max(1.0, tiles - 0.5 * max_q / kWdTile);   // tiles of a unit, on average, when causal
+    const double gain = wide_seqs * c->kv_heads * (1.1 / c->sm_count * per_head * seen - 0.02 * tiles);
     const size_t tile_bytes = 2 * static_cast<size_t>(kWdTile) * c->head_dim * 2;
     const size_t copy = static_cast<size_t>(batch) * c->kv_heads * std::max<int64_t>(1, tiles) * tile_bytes;
+    const int force = g_force_attention_copy.load(std::memory_order_relaxed);
     a->max_tiles = static_cast<int>(std::max<int64_t>(1, tiles));
-    a->ready = per_head >= kReadyUnits && copy <= kReadyBytes && a->max_tiles <= 65535 * 16 && batch <= 65535 && c->kv_heads <= 65535;
+    a->ready = force != 1 && (gain > 7.0 || force == 2) && copy <= kReadyBytes;
     if (a->ready) {
       a->ready_tiles = round_up(a->bytes, 1024);
       a->ready_info = a->ready_tiles + copy;
@@ -2504,6 +2511,7 @@ int32_t batq_debug_gemm_choice(int64_t s, int64_t m, int64_t n, int32_t sm_count
   if (width != nullptr) *width = bn;
   return kernel;
 }
+void batq_debug_force_attention_copy(int32_t which) { g_force_attention_copy.store(which, std::memory_order_relaxed); }
 void batq_debug_force_quantizer(int32_t which) { g_force_quantizer.store(which, std::memory_order_relaxed); }
 void batq_debug_force_gemm_kernel(int32_t which) { g_force_gemm_kernel.store(which, std::memory_order_relaxed); }
 void batq_debug_force_small_s_splits(int32_t splits) { g_force_splits.store(splits, std::memory_order_relaxed); }
@@ -2786,7 +2794,7 @@ size_t batq_attention_kv_mxfp8_workspace_bytes(const batq_kv_cache* c, int32_t q
   if (c == nullptr || q_heads <= 0 || q_heads % c->kv_heads != 0 || tokens < 0 || seqs < 0 || max_q <= 0 || max_kv < 0) return 0;
   if (tokens == 0 || seqs == 0) return 0;
   AttnPlan a;
-  return plan_attention(c, q_heads, seqs, max_q, max_kv, &a) ? a.bytes : 0;
+  return plan_attention(c, q_heads, tokens, seqs, max_q, max_kv, &a) ? a.bytes : 0;
 }
 
 batq_status batq_attention_kv_mxfp8(const batq_kv_cache* c, const void* q_bf16, int64_t ldq, int32_t q_heads, int64_t tokens,
@@ -2806,7 +2814,7 @@ batq_status batq_attention_kv_mxfp8(const batq_kv_cache* c, const void* q_bf16, 
   if (st != BATQ_OK) return st;
   if (!aligned(q_starts, 4) || !aligned(kv_lens, 4) || !aligned(page_table, 4) || !aligned(lse, 4)) return BATQ_ERR_ALIGN;
   AttnPlan a;
-  if (!plan_attention(c, q_heads, seqs, max_q, max_kv, &a)) return BATQ_ERR_SHAPE;
+  if (!plan_attention(c, q_heads, tokens, seqs, max_q, max_kv, &a)) return BATQ_ERR_SHAPE;
   if (a.bytes > 0) {
     if (workspace == nullptr) return BATQ_ERR_NULL;
     if (!aligned(workspace, 256)) return BATQ_ERR_ALIGN;

@@ -94,6 +94,14 @@ class Batch:
         assert (out[n:] == 7.0).all() and (lse is None or (lse[n:] == 5.0).all())
 
 
+@pytest.fixture(params=[1, 2], ids=["codes", "copy"])
+def copy_path(batq, request):
+    """Prompts from the codes, or from the f16 copy in the workspace, whatever the call's sizes would choose."""
+    batq.batq_debug_force_attention_copy(request.param)
+    yield request.param
+    batq.batq_debug_force_attention_copy(0)
+
+
 HEADS = [(32, 8, 128), (28, 4, 128), (3, 3, 128), (12, 1, 128), (16, 4, 64), (5, 5, 64), (20, 2, 64)]
 
 
@@ -125,7 +133,7 @@ def test_several_rows(batq, heads, kv_heads, d, causal):
 @pytest.mark.parametrize("heads,kv_heads,d,page", [(32, 8, 128, 64), (28, 4, 128, 16), (12, 1, 128, 128), (16, 4, 64, 32), (3, 3, 64, 16)])
 @pytest.mark.parametrize("causal", [True, False])
 @pytest.mark.parametrize("rows,lens", [([129], [129]), ([1, 77, 300, 1], [513, 78, 300, 1]), ([64], [1500]), ([200, 31], [150, 31])])
-def test_prompts(batq, heads, kv_heads, d, page, causal, rows, lens):
+def test_prompts(batq, heads, kv_heads, d, page, causal, rows, lens, copy_path):
     """Whole prompts, chunks behind a context, more rows than keys."""
     b = Batch(batq, heads, kv_heads, d, page, rows, lens, seed=4, extra_q=2)
     b.check(*b.run(batq, causal=causal), causal=causal)
@@ -140,28 +148,35 @@ def test_more_sequences_than_one_launch(batq):
     b.check(*b.run(batq, use_starts=False))
 
 
-def test_prompt_beside_decoding(batq):
+def test_prompt_beside_decoding(batq, copy_path):
     rows, lens = [1] * 6 + [173] + [1] * 3, [900, 3, 64, 65, 0, 511, 700, 1, 1025, 33]
     b = Batch(batq, 32, 8, 128, 64, rows, lens, seed=5)
     b.check(*b.run(batq))
 
 
 @pytest.mark.parametrize("rows", [[1, 1, 1], [40, 1, 19]])
-def test_bounds_may_be_larger_than_the_batch(batq, rows):
+def test_bounds_may_be_larger_than_the_batch(batq, rows, copy_path):
     """max_q and max_kv size the grid only; a captured call meets other lengths within them."""
     b = Batch(batq, 32, 8, 128, 64, rows, [700, 64, 19], seed=6)
     b.check(*b.run(batq, max_q=300, max_kv=20000))
 
 
-@pytest.mark.parametrize("max_kv,ready", [(700, True), (200000, False)])
-def test_keys_widened_once_or_by_every_unit(batq, max_kv, ready):
-    """Prompts of several units: from an f16 copy in the workspace, or where that would be too large (200000 keys for
-    each of three sequences) from the codes; both against the definition."""
+def test_where_keys_are_widened_once(batq):
+    """The copy is in the workspace of large prompts, not of small or of huge ones (max_kv is a bound: the grid's alone)."""
     b = Batch(batq, 32, 8, 128, 64, [150, 1, 77], [700, 64, 77], seed=20)
-    n = batq.batq_attention_kv_mxfp8_workspace_bytes(b.cache, 32, 228, 3, 150, max_kv)
-    copy = 3 * 8 * -(-max_kv // 128) * 65536
-    assert (n >= copy) == ready
-    b.check(*b.run(batq, max_kv=max_kv))
+
+    def copied(*sizes):
+        """Bytes of workspace beyond what the call wants without a copy."""
+        batq.batq_debug_force_attention_copy(1)
+        least = batq.batq_attention_kv_mxfp8_workspace_bytes(b.cache, 32, *sizes)
+        batq.batq_debug_force_attention_copy(0)
+        return batq.batq_attention_kv_mxfp8_workspace_bytes(b.cache, 32, *sizes) - least
+
+    copy = lambda seqs, max_kv: seqs * 8 * -(-max_kv // 128) * 65536  # noqa: E731
+    assert copied(2048, 1, 2048, 2048) >= copy(1, 2048)
+    assert copied(8 * 512, 8, 512, 8192) >= copy(8, 8192)
+    assert copied(64, 1, 64, 8192) == copied(100000, 1, 100000, 200000) == copied(228, 3, 150, 200000) == 0
+    b.check(*b.run(batq, max_kv=200000))
 
 
 @pytest.mark.parametrize("rows", [1, 5, 70])
@@ -186,7 +201,7 @@ def test_lengths_beyond_the_bounds_are_not_looked_at(batq):
     b.check(got[3:], None)
 
 
-def test_scale_and_gain(batq):
+def test_scale_and_gain(batq, copy_path):
     """A scale of the caller's; sharp and flat distributions; queries and values of very different sizes."""
     for scale, gain in ((1.0, 1.0), (0.01, 30.0), (-0.2, 1.0), (0.0, 1.0)):
         b = Batch(batq, 16, 4, 64, 16, [1, 6], [300, 90], seed=9, gain=gain)
@@ -197,7 +212,7 @@ def test_scale_and_gain(batq):
 
 
 @pytest.mark.parametrize("rows", [1, 50])
-def test_value_scales_far_apart(batq, rows):
+def test_value_scales_far_apart(batq, rows, copy_path):
     """A token with huge values and next to no weight, a token with all the weight and tiny values, blocks of zeros."""
     b = Batch(batq, 8, 2, 128, 32, [rows], [400], seed=11, spread=0.1)
     kc, ks = b.k
@@ -213,7 +228,7 @@ def test_value_scales_far_apart(batq, rows):
     b.check(*b.run(batq))
 
 
-def test_strides_and_in_between_columns(batq):
+def test_strides_and_in_between_columns(batq, copy_path):
     """q and out as column ranges of wider tensors; what lies beside them stays."""
     b = Batch(batq, 8, 2, 128, 32, [1, 3, 40], [77, 40, 100], seed=12)
     wide = torch.full((44, 8 * 128 + 24), 3.0, dtype=torch.bfloat16, device="cuda")
@@ -226,7 +241,7 @@ def test_strides_and_in_between_columns(batq):
 
 @pytest.mark.parametrize("page", [16, 64])
 @pytest.mark.parametrize("rows", [1, 45])
-def test_bad_pages_are_left_out_and_reported(batq, page, rows):
+def test_bad_pages_are_left_out_and_reported(batq, page, rows, copy_path):
     b = Batch(batq, 8, 4, 64, page, [rows, rows], [200, 150], seed=13)
     hidden = [torch.zeros(200, dtype=torch.bool), torch.zeros(150, dtype=torch.bool)]
     for seq, at, bad in ((0, 1, -1), (1, 0, b.buffers[0].shape[0]), (1, 1, 1 << 30)):
@@ -253,7 +268,7 @@ def test_row_starts_out_of_order_stay_inside(batq):
 
 
 @pytest.mark.parametrize("rows", [[1, 1, 1, 1], [3, 1, 70, 2]])
-def test_captured_and_replayed_with_other_lengths(batq, rows):
+def test_captured_and_replayed_with_other_lengths(batq, rows, copy_path):
     """One capture, replayed after the lengths, the page table and the queries have changed; on a stream of its own."""
     b = Batch(batq, 32, 8, 128, 64, rows, [600, 40, 130, 2000], seed=15)
     q, out, lse = b.q.cuda().flatten(1), torch.full((sum(rows), 4096), 7.0, dtype=torch.bfloat16, device="cuda"), torch.zeros(sum(rows), 32, device="cuda")
@@ -273,7 +288,7 @@ def test_captured_and_replayed_with_other_lengths(batq, rows):
         b.check(out.unflatten(1, (32, 128)), lse)
 
 
-def test_same_bits_again_and_on_two_streams(batq):
+def test_same_bits_again_and_on_two_streams(batq, copy_path):
     """Repeated and concurrent calls give the same bits."""
     b = Batch(batq, 28, 4, 128, 64, [1, 1, 40, 2], [5000, 100, 300, 900], seed=16)
     first, lse = b.run(batq)
