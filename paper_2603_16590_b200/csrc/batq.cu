@@ -1714,8 +1714,9 @@ cudaError_t launch_append(int gc, int grid, const KvAppendParams& p, cudaStream_
 
 // How a call of the attention is cut.  Sequences with up to kNarrowRows rows (query rows x heads of the group) go to
 // attention_kv_kernel, the others to attention_kv_wide_kernel; a call of one sequence that may have more makes one
-// launch only.
-constexpr int kNarrowRows = 32;
+// launch only.  Both sides, 32 / 8 heads: 48 rows of 1 / 8 / 32 sequences behind 8192 keys 31 / 90 / 289 us against 42 / 128 /
+// 424; 64 rows (in units of 16) 29 / 122 / 439 against 42 / 129 / 427, and of 32 sequences behind 1024 keys 92 against 82.
+constexpr int kNarrowRows = 48;
 constexpr size_t kReadyBytes = size_t(512) << 20;   // most that the f16 copy of K and V may take
 std::atomic<int> g_force_attention_copy{0};         // tuning hook: 0 = automatic, 1 = never, 2 = wherever it fits
 struct AttnPlan {
@@ -1737,7 +1738,9 @@ bool plan_attention(const batq_kv_cache* c, int32_t q_heads, int64_t tokens, int
   a->narrow = !a->wide || seqs > 1;
   if (a->narrow) {
     const int64_t rows = std::min<int64_t>(most, kNarrowRows);
-    a->nt = rows <= 8 ? 1 : rows <= 16 || rows > 24 ? 2 : 3;   // as few units as can be; more rows than 24 of one do not fit the registers
+    // As few units as can be, of 8, 16 or 24 rows (more of one do not fit the registers): 24 sequences of up to 20 rows
+    // one unit of 24 21.2 us, two of 16 22.3.  Beside prompts most of the others decode: 16.
+    a->nt = rows <= 8 ? 1 : !a->wide && (rows + 23) / 24 < (rows + 15) / 16 ? 3 : 2;
     const int64_t units = (rows + 8 * a->nt - 1) / (8 * a->nt) * c->kv_heads * batch;
     const int64_t tiles = std::max<int64_t>(1, (static_cast<int64_t>(max_kv) + kAtTile - 1) / kAtTile);
     if (units > INT_MAX || units * (tiles + kAtUnitCost) > INT_MAX) return false;   // the kernel counts tiles in 32 bits

@@ -132,7 +132,8 @@ def test_several_rows(batq, heads, kv_heads, d, causal):
 
 @pytest.mark.parametrize("heads,kv_heads,d,page", [(32, 8, 128, 64), (28, 4, 128, 16), (12, 1, 128, 128), (16, 4, 64, 32), (3, 3, 64, 16)])
 @pytest.mark.parametrize("causal", [True, False])
-@pytest.mark.parametrize("rows,lens", [([129], [129]), ([1, 77, 300, 1], [513, 78, 300, 1]), ([64], [1500]), ([200, 31], [150, 31])])
+@pytest.mark.parametrize("rows,lens", [([129], [129]), ([1, 77, 300, 1], [513, 78, 300, 1]), ([64], [1500]), ([200, 31], [150, 31]),
+                                       ([12, 8, 3], [700, 9, 40])])
 def test_prompts(batq, heads, kv_heads, d, page, causal, rows, lens, copy_path):
     """Whole prompts, chunks behind a context, more rows than keys."""
     b = Batch(batq, heads, kv_heads, d, page, rows, lens, seed=4, extra_q=2)
