@@ -352,7 +352,7 @@ batq_status batq_kv_append_mxfp8(const batq_kv_cache* c, const batq_transform* t
  *   page_table   dev int32 [seqs x ld_pages]: the pages of each sequence in the order of its tokens.  Entries behind
  *                a sequence's last page are not read.  A page outside the pool: its keys are left out and the next
  *                batq_last_device_status returns BATQ_ERR_INDEX.
- *   max_q        no sequence has more query rows; max_kv: none has more keys.  Bounds that size the grid and the
+ *   max_q        no sequence has more query rows; max_kv (<= 2^30): none has more keys.  Bounds that size the grid and the
  *                workspace (a captured call is replayed with other lengths within them); what a sequence has beyond
  *                them, or beyond ld_pages * page_size keys, is not looked at.
  *   lse          dev fp32 [tokens x q_heads] or NULL.

@@ -2794,7 +2794,7 @@ batq_status batq_kv_append_mxfp8(const batq_kv_cache* c, const batq_transform* t
 
 size_t batq_attention_kv_mxfp8_workspace_bytes(const batq_kv_cache* c, int32_t q_heads, int64_t tokens, int32_t seqs,
                                                int32_t max_q, int32_t max_kv) {
-  if (c == nullptr || q_heads <= 0 || q_heads % c->kv_heads != 0 || tokens < 0 || seqs < 0 || max_q <= 0 || max_kv < 0) return 0;
+  if (c == nullptr || q_heads <= 0 || q_heads % c->kv_heads != 0 || tokens < 0 || seqs < 0 || max_q <= 0 || max_kv < 0 || max_kv > (1 << 30)) return 0;
   if (tokens == 0 || seqs == 0) return 0;
   AttnPlan a;
   return plan_attention(c, q_heads, tokens, seqs, max_q, max_kv, &a) ? a.bytes : 0;
@@ -2807,7 +2807,7 @@ batq_status batq_attention_kv_mxfp8(const batq_kv_cache* c, const void* q_bf16, 
                                     void* stream) {
   if (c == nullptr) return BATQ_ERR_NULL;
   if (q_heads <= 0 || q_heads % c->kv_heads != 0 || q_heads > kKvMaxHeads || tokens < 0 || tokens > (int64_t(1) << 30) || seqs < 0 ||
-      max_q <= 0 || max_kv < 0 || ld_pages < 0 || !std::isfinite(scale))
+      max_q <= 0 || max_kv < 0 || max_kv > (1 << 30) || ld_pages < 0 || !std::isfinite(scale))
     return BATQ_ERR_SHAPE;
   if (q_starts == nullptr && tokens != seqs) return BATQ_ERR_SHAPE;
   if (seqs == 0 || tokens == 0) return BATQ_OK;

@@ -321,6 +321,7 @@ def test_attention_refuses(batq):
     _refused(batq, SHAPE, lambda: call(starts=None))                     # one row per sequence: 5 rows, 2 sequences
     _refused(batq, SHAPE, lambda: call(max_q=0))
     _refused(batq, SHAPE, lambda: call(max_kv=-1))
+    _refused(batq, SHAPE, lambda: call(max_kv=(1 << 30) + 1))
     _refused(batq, SHAPE, lambda: call(scale=math.nan))
     _refused(batq, SHAPE, lambda: call(q=q[:, :384], out=out[:, :384]))                    # 3 heads over 2
     _refused(batq, SHAPE, lambda: call(q=torch.zeros(1024, dtype=torch.bfloat16, device="cuda").expand(5, 1024)))
