@@ -361,9 +361,14 @@ batq_status batq_kv_append_mxfp8(const batq_kv_cache* c, const batq_transform* t
  *                for decoding, up to 40 MB for prompts; where prompts pay for it, also an f16 copy of the keys and values,
  *                seqs * max_kv * kv_heads * head_dim * 4 bytes, at most 512 MB.
  * Repeated, a call gives the same bits: nothing depends on the order in which parts finish.  The last bits of a row may
- * depend on the lengths of the other sequences, which move the places where long sequences are divided.  Finite q, keys
- * and values; a value that is more than 2^28 smaller than the largest of the 128 tokens it stands with (tokens 128 i to
- * 128 i + 127 of a sequence) is rounded to a multiple of 2^-40 of that.  seqs == 0 or tokens == 0 is a no-op.
+ * depend on the lengths of the other sequences, which move the places where long sequences are divided.
+ * Finite q, keys and values.  Scores and sums are fp32.  Softmax weights are f16: off by 2^-11 of themselves, or by
+ * 2^-24 of the row's largest p_t |v_t| over this |v_t| where that is more, with |v_t| the largest element of token t's
+ * values, 2^-49 at least.  Keys and values are exact, but in these cases: values below 2^-85 count as multiples of 2^-88;
+ * a value more than 2^28 smaller than |v_t| as a multiple of 2^-31 of it; with more than 48 rows (query rows x heads of the group) a
+ * key's element more than 2^28 smaller than the largest of the 128 tokens it stands with (tokens 128 i to 128 i + 127 of a
+ * sequence) as a multiple of 2^-39 of that.  Where values pass 2^64, tokens without any may lose their share of p.
+ * seqs == 0 or tokens == 0 is a no-op.
  * Errors: NULL / SHAPE / ALIGN / UNSUPPORTED / WORKSPACE / CUDA. */
 size_t batq_attention_kv_mxfp8_workspace_bytes(const batq_kv_cache* c, int32_t q_heads, int64_t tokens, int32_t seqs,
                                                int32_t max_q, int32_t max_kv);

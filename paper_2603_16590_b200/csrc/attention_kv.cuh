@@ -18,11 +18,11 @@
 // the codes would still have to be widened.  E4M3 is exact in f16; the scales are kept apart from it:
 //   scores   S = sum_b 2^ek[t,b] (q_b . kc_b): one fp32 factor per token and block on the accumulators.  q is scaled by
 //            a power of two per row so that its largest element is in [2^14, 2^15): exact in f16 down to 2^-31 of it.
-//   values   vc 2^(ev - c) in f16 with c one integer per tile (its largest ev, less 7): exact within 2^22 of the tile's
-//            largest block.  c joins the exponent of the softmax weight, w = 2^(s + c - m) with m the running maximum
-//            of s + c, so that w is exact to f16 relative to the largest *contribution* to the output, not to the
-//            largest probability: a token of large probability and tiny values (an attention sink) costs no precision.
-//            The softmax sum takes 2^-c w in fp32.
+//   values   vc 2^(ev - c) in f16 with c one integer per token (its largest ev, less 7): exact within 2^22 of the token's
+//            largest block.  c joins the exponent of the softmax weight, w = 2^(s + c - m) with m the reference, 2^7 below
+//            the row's largest s + c when it was set.  So w, in f16, is off by 2^-11 of itself or by 2^-32 of the row's
+//            largest *contribution* to the output, not of its largest probability: a token of large probability and tiny
+//            values (an attention sink) leaves the others their bits.  The softmax sum takes 2^-c w in fp32.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -38,9 +38,11 @@ constexpr int kAtStages = 2;       // x 8.4 KB x 4 warps: three CTAs on an SM
 constexpr int kAtSnap = 8;        // units of up to this many tiles are not divided
 constexpr int kAtMaxSeqs = 512;   // sequences of one launch
 constexpr int kAtUnitCost = 12;   // what a unit costs besides its tiles, in tiles (look-ups, first loads, the merge; 6: 115 us, 8: 113, 12: 110 for 128 ragged sequences)
-constexpr float kAtSlack = 8.0f;  // how far (log2) a score may stand above the reference: weights up to 2^8 in f16
+constexpr float kAtHead = 7.0f;   // log2 of a row's largest weight when its reference is set: f16 has no bits below 2^-24
+constexpr float kAtMost = 15.0f;  // log2 of the largest weight that leaves the reference where it is: f16 ends at 2^16
 constexpr float kAtNone = -1e30f; // the reference of a row that has seen no key
-constexpr int kAtMinScale = -32;  // least c: an all-zero tile must not push the softmax sum's terms out of fp32
+// Least c: 2^-c times a weight is a term of the softmax sum in fp32, of tokens without any value too.
+constexpr int kAtMinScale = -64;
 
 struct AttnJoin {
   int32_t parts;     // CTAs that share the unit, this one among them; 0: none starts here
@@ -71,7 +73,7 @@ struct AttnParams {
   int32_t most_rows;          // sequences with more rows (query rows x group) are another kernel's
   int32_t seq0;               // row of its first sequence where q_starts is NULL
   float* part_o;              // [CTA][2][rows][head_dim]: sums relative to part_ml's reference
-  float2* part_ml;            // [CTA][2][rows]: reference exponent m, softmax sum
+  float2* part_ml;            // [CTA][2][rows]: reference m, softmax sum
   AttnJoin* join;             // [CTA]: the unit that starts in its range and ends in another's
 };
 
@@ -84,7 +86,7 @@ struct AttnCfg {
   static constexpr int kScaleBytes = kAtTile * kBlocks;            // of K or V
   static constexpr int kRing = kAtWarps * kAtStages * kStageBytes;
   static constexpr int kScales = kAtWarps * kAtStages * 2 * kScaleBytes;
-  static constexpr int kMult = kAtWarps * kBlocks * kAtTile * 2;   // 2^(ev - c) of a warp's tile, f16
+  static constexpr int kMult = kAtWarps * kBlocks * kAtTile * 2;   // 2^(ev - c) of the tokens of a warp's tile, f16
   static constexpr int kKeyMult = kAtWarps * kBlocks * kAtTile * 4; // 2^ek, fp32
   static constexpr int kSmemBytes = kRing + kScales + kMult + kKeyMult + 1024;
   static constexpr int kCtasPerSm = NT == 1 ? 3 : 2;   // by shared memory; by registers
@@ -159,6 +161,10 @@ __device__ __forceinline__ float ex2(float x) {   // results below 2^-126 are 0:
 }
 __device__ __forceinline__ float pow2i(int e) {   // 2^e, e in [-126, 127]
   return __int_as_float((e + 127) << 23);
+}
+__device__ __forceinline__ uint32_t largest_byte(uint32_t w) {
+  const uint32_t top = __vmaxu4(w, w >> 16);
+  return max(top & 255u, (top >> 8) & 255u);
 }
 // 2^e as f16 bits; 0 below 2^-24 (e <= 7 here).
 __device__ __forceinline__ uint32_t f16_pow2(int e) {
@@ -445,8 +451,8 @@ attention_kv_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
             asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(vt + lane * D + c * 16), "r"(0u) : "memory");
         }
       }
-      // the value scales of the lane's token, the tile's common exponent, and the f16 factors 2^(ev - c)
-      int c_tile;
+      // the value scales of the lane's token, their common exponent, and the f16 factors 2^(ev - c)
+      int c_lane;
       {
         uint32_t w;
         if (BL == 4) w = *reinterpret_cast<const uint32_t*>(vs + lane * 4);
@@ -460,13 +466,11 @@ attention_kv_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
         if (BL == 4) *reinterpret_cast<uint4*>(kmult + lane * 4) = make_uint4(kf[0], kf[1], kf[BL - 2], kf[BL - 1]);
         else *reinterpret_cast<uint2*>(kmult + lane * 2) = make_uint2(kf[0], kf[1]);
         if (!here) w = 0;
-        uint32_t top = __vmaxu4(w, w >> 16);
-        top = __reduce_max_sync(0xFFFFFFFFu, max(top & 255u, (top >> 8) & 255u));
-        c_tile = max(static_cast<int>(top) - 127 - 7, kAtMinScale);
+        c_lane = max(static_cast<int>(largest_byte(w)) - 127 - 7, kAtMinScale);
         const int at = (lane & 24) | token_frag<D>(lane & 7);
 #pragma unroll
         for (int b = 0; b < BL; b += 2) {   // two blocks in the halves of a word
-          const uint32_t f = f16_pow2x2(__byte_perm(w, 0u, b == 0 ? 0x4140 : 0x4342), c_tile + 127);
+          const uint32_t f = f16_pow2x2(__byte_perm(w, 0u, b == 0 ? 0x4140 : 0x4342), c_lane + 127);
           mult[b * kAtTile + at] = static_cast<uint16_t>(f);
           mult[(b + 1) * kAtTile + at] = static_cast<uint16_t>(f >> 16);
         }
@@ -505,20 +509,26 @@ attention_kv_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
           }
         }
       }
-      // Weights against the reference m: it follows the maximum only where a score is more than 2^8 above it, so that
+      // Weights against the reference m: it follows the maximum only where that has grown by more than 2^8, so that
       // most tiles exchange nothing between the lanes and leave the accumulators alone.
-      const float cf = static_cast<float>(c_tile);
+      float cf[2][2], unscale[2][2];   // c, 2^-c of the thread's four tokens
+#pragma unroll
+      for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int c = __shfl_sync(0xFFFFFFFFu, c_lane, mt * 16 + h * 8 + frag_token<D>(g));
+          cf[mt][h] = static_cast<float>(c);
+          unscale[mt][h] = pow2i(-c);
+        }
       float z[2][NT][4];
       auto weigh = [&] {   // exponents of the weights; returns the largest
         float top = -INFINITY;
 #pragma unroll
         for (int j = 0; j < NT; ++j)
 #pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            const float t = cf - m[j][x & 1];
+          for (int x = 0; x < 4; ++x)
 #pragma unroll
-            for (int mt = 0; mt < 2; ++mt) z[mt][j][x] = fmaf(s[mt][j][x], qs[j][x & 1], t);
-          }
+            for (int mt = 0; mt < 2; ++mt) z[mt][j][x] = fmaf(s[mt][j][x], qs[j][x & 1], cf[mt][x >> 1] - m[j][x & 1]);
         if (!whole) {
 #pragma unroll
           for (int j = 0; j < NT; ++j)
@@ -536,7 +546,7 @@ attention_kv_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
           for (int x = 0; x < 4; ++x) top = fmaxf(top, fmaxf(z[0][j][x], z[1][j][x]));
         return top;
       };
-      if (__any_sync(0xFFFFFFFFu, weigh() > kAtSlack)) {
+      if (__any_sync(0xFFFFFFFFu, weigh() > kAtMost)) {
 #pragma unroll
         for (int j = 0; j < NT; ++j)
 #pragma unroll
@@ -546,11 +556,11 @@ attention_kv_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
             for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
               for (int h = 0; h < 2; ++h)
-                if (z[mt][j][x + 2 * h] > -INFINITY) top = fmaxf(top, fmaf(s[mt][j][x + 2 * h], qs[j][x], cf));
+                if (z[mt][j][x + 2 * h] > -INFINITY) top = fmaxf(top, fmaf(s[mt][j][x + 2 * h], qs[j][x], cf[mt][h]));
             top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 4));
             top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 8));
             top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 16));
-            const float mn = fmaxf(m[j][x], top), alpha = ex2(m[j][x] - mn);
+            const float mn = fmaxf(m[j][x], top - kAtHead), alpha = ex2(m[j][x] - mn);
             m[j][x] = mn;
             l[j][x] *= alpha;
 #pragma unroll
@@ -562,7 +572,6 @@ attention_kv_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
         weigh();
       }
       uint32_t pf[2][NT][2];
-      const float unscale = pow2i(max(-c_tile, -126));
 #pragma unroll
       for (int j = 0; j < NT; ++j) {
 #pragma unroll
@@ -572,9 +581,10 @@ attention_kv_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
           for (int mt = 0; mt < 2; ++mt) {
             z[mt][j][x] = ex2(z[mt][j][x]);
             z[mt][j][x + 2] = ex2(z[mt][j][x + 2]);
-            sum += z[mt][j][x] + z[mt][j][x + 2];
+            sum = fmaf(z[mt][j][x], unscale[mt][0], sum);
+            sum = fmaf(z[mt][j][x + 2], unscale[mt][1], sum);
           }
-          l[j][x] = fmaf(sum, unscale, l[j][x]);
+          l[j][x] += sum;
         }
 #pragma unroll
         for (int mt = 0; mt < 2; ++mt)

@@ -12,7 +12,9 @@
 //                  so O is hardly ever read back before the end.
 //   the others     one warp brings tiles, one issues the MMAs, and without READY four widen the codes: K 2^(ek - ck) and
 //                  V 2^(ev - cv) in f16, ck and cv one integer per 128 tokens, into 128-byte-swizzled tiles (K: K-major B
-//                  operand; V: MN-major B operand, the same bytes).  The block-scaled kinds would take the codes as they
+//                  operand; V: MN-major B operand, the same bytes).  Where a token's values are more than 2^kWdEven
+//                  smaller than the tile's largest, each token has its own cv, as in attention_kv.cuh: its weights
+//                  would else count against the reference with the size of its neighbours' values.  The block-scaled kinds would take the codes as they
 //                  are, but want q and P in 8 bits, and V's scales along the wrong axis.
 //
 // What bounds it is instruction issue beside the exponentials: on each of an SM's four schedulers two softmax warps (some
@@ -28,6 +30,7 @@
 // Units go to the CTAs (one per SM) longest first, alternately up and down.  Where there are few, each is divided along
 // its tokens into as many parts as finish soonest; attention_wide_join_kernel adds the parts up in order.
 #pragma once
+#include <cstddef>
 #include <type_traits>
 
 #include "attention_kv.cuh"
@@ -38,6 +41,7 @@ namespace batq {
 
 constexpr int kWdRows = 256;        // of a unit
 constexpr int kWdTile = 128;        // tokens
+constexpr int kWdEven = 8;          // log2: weights are within 2^(kWdEven - 32) of the row's largest contribution
 constexpr int kWdPartCost = 4;      // what a part of a unit costs besides its tiles, in tiles
 
 struct AttnWidePlan { int32_t units, splits; };
@@ -54,11 +58,17 @@ struct AttnWideShape {
 };
 
 // What the softmax has to know of a tile.
-struct AttnTileInfo {
-  int32_t ck, cv;       // the exponents that its keys and values have been divided by
-  uint32_t missing;     // 16-token pieces of it whose page is not there
-  int32_t pad;
+struct __align__(16) AttnTileInfo {
+  int32_t ck, cv;        // the exponents that its keys and values have been divided by
+  uint32_t missing;      // 16-token pieces of it whose page is not there
+  int32_t uneven;        // != 0: token i's values by cv - less[i] (else less is 0)
+  uint8_t less[kWdTile];
 };
+static_assert(sizeof(AttnTileInfo) % 16 == 0 && offsetof(AttnTileInfo, less) == 16, "copied by bulk_g2s; its head read as an int4");
+// The exponent of a tile's values, or of one token's, from its largest scale byte; how much less a token's is.
+__device__ __forceinline__ int attn_value_exponent(uint32_t top) { return max(static_cast<int>(top) - 127 - 7, kAtMinScale); }
+__device__ __forceinline__ bool attn_uneven(uint32_t top, uint32_t low) { return attn_value_exponent(top) - attn_value_exponent(low) > kWdEven; }
+__device__ __forceinline__ int attn_less(int cv, uint32_t own) { return max(cv - attn_value_exponent(own), 0); }
 
 struct AttnWideParams {
   AttnParams a;
@@ -336,8 +346,10 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
         if (!ok) break;
         s_phase ^= 1u;
         tc_fence_after_sync();
-        const AttnTileInfo ex = info[(turn + j) % Cfg::kScaleSlots];
-        const uint32_t miss = ex.missing;
+        const AttnTileInfo& tile = info[(turn + j) % Cfg::kScaleSlots];
+        const int4 ex = *reinterpret_cast<const int4*>(&tile);   // ck, cv, missing, uneven
+        const uint32_t miss = static_cast<uint32_t>(ex.z);
+        const bool uneven = ex.w != 0;
         const int tok0 = (it.tile0 + j) * kWdTile, see = lim - tok0;
         const bool part = tok0 + kWdTile > full || miss != 0;
         uint32_t s[4][32];
@@ -359,6 +371,21 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
                 if ((miss >> (c * 2 + (i >> 4))) & 1u) s[c][i] = 0xFF800000u;
           }
         }
+        float qk = fmaxf(qs * pow2i(max(ex.x, -126)), 1e-37f);
+        const float cv = static_cast<float>(ex.y);
+        if (uneven) {   // each token's score with its own exponent, relative to the tile's
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int i = 0; i < 32; i += 4) {
+              const uchar4 d = *reinterpret_cast<const uchar4*>(&tile.less[c * 32 + i]);
+              s[c][i] = __float_as_uint(fmaf(__uint_as_float(s[c][i]), qk, -static_cast<float>(d.x)));
+              s[c][i + 1] = __float_as_uint(fmaf(__uint_as_float(s[c][i + 1]), qk, -static_cast<float>(d.y)));
+              s[c][i + 2] = __float_as_uint(fmaf(__uint_as_float(s[c][i + 2]), qk, -static_cast<float>(d.z)));
+              s[c][i + 3] = __float_as_uint(fmaf(__uint_as_float(s[c][i + 3]), qk, -static_cast<float>(d.w)));
+            }
+          qk = 1.0f;
+        }
         float tops[4];   // four chains: one takes 10 cycles a step
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
@@ -367,9 +394,8 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
           for (int i = 1; i < 32; ++i) tops[c] = fmaxf(tops[c], __uint_as_float(s[c][i]));
         }
         const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-        const float qk = fmaxf(qs * pow2i(max(ex.ck, -126)), 1e-37f), cv = static_cast<float>(ex.cv);
-        if (__any_sync(0xFFFFFFFFu, fmaf(top, qk, cv - m) > kAtSlack)) {
-          const float mn = fmaxf(m, fmaf(top, qk, cv)), alpha = ex2(m - mn);
+        if (__any_sync(0xFFFFFFFFu, fmaf(top, qk, cv - m) > kAtMost)) {
+          const float mn = fmaxf(m, fmaf(top, qk, cv) - kAtHead), alpha = ex2(m - mn);
           m = mn;
           l *= alpha;
           if (j > 0) {   // the value product of the tile before is done: its S was waited for
@@ -386,25 +412,34 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
         }
         const uint64_t qk2 = f32x2_pack(qk, qk), t2 = f32x2_pack(cv - m, cv - m);
         uint64_t sum0 = 0, sum1 = 0;
+        auto weigh = [&](auto per_token) {   // the weights, to where the scores were, and their sum
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          const uint32_t (&x)[32] = s[c];
-          uint32_t w[16];
+          for (int c = 0; c < 4; ++c) {
+            const uint32_t (&x)[32] = s[c];
+            uint32_t w[16];
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            float a, b;
-            f32x2_unpack(f32x2_fma(f32x2_pack(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), qk2, t2), a, b);
-            a = ex2(a);
-            b = ex2(b);
-            if (i & 1) sum1 = f32x2_add(sum1, f32x2_pack(a, b));
-            else sum0 = f32x2_add(sum0, f32x2_pack(a, b));
-            w[i] = f16x2_pack(a, b);
+            for (int i = 0; i < 16; ++i) {
+              float a, b;
+              f32x2_unpack(f32x2_fma(f32x2_pack(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), qk2, t2), a, b);
+              a = ex2(a);
+              b = ex2(b);
+              uint64_t& sum = i & 1 ? sum1 : sum0;
+              if (per_token.value) {
+                const uchar2 d = *reinterpret_cast<const uchar2*>(&tile.less[c * 32 + 2 * i]);
+                sum = f32x2_fma(f32x2_pack(a, b), f32x2_pack(pow2i(d.x - ex.y), pow2i(d.y - ex.y)), sum);
+              } else {
+                sum = f32x2_add(sum, f32x2_pack(a, b));
+              }
+              w[i] = f16x2_pack(a, b);
+            }
+            tmem_st_32x32b_x16(s_at + c * 16, w);
           }
-          tmem_st_32x32b_x16(s_at + c * 16, w);
-        }
+        };
+        if (uneven) weigh(std::true_type{});
+        else weigh(std::false_type{});
         float a, b;
         f32x2_unpack(f32x2_add(sum0, sum1), a, b);
-        l = fmaf(a + b, pow2i(max(-ex.cv, -126)), l);
+        l = fmaf(a + b, uneven ? 1.0f : pow2i(-ex.y), l);
         tmem_st_wait();
         tc_fence_before_sync();
         __syncwarp();
@@ -491,7 +526,7 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
         const uint8_t* vs = ks + Cfg::kScaleBytes;
         int cs[2];
         uint32_t miss = 0;
-        bool cut = false;
+        bool cut = false, uneven = false;
 #pragma unroll
         for (int v = 0; v < 2; ++v, ++n_step) {   // K, then V
           const uint32_t st = n_step % kStages, phase = (n_step / kStages) & 1u;
@@ -507,30 +542,29 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
               const uint8_t* src = x == 0 ? ks : vs;
-              uint32_t top = 0;
-              if (!cut) {
-                if (BL == 4) {
-                  const uint4 w = *reinterpret_cast<const uint4*>(src + lane * 16);
-                  top = __vmaxu4(__vmaxu4(w.x, w.y), __vmaxu4(w.z, w.w));
-                } else {
-                  const uint2 w = *reinterpret_cast<const uint2*>(src + lane * 8);
-                  top = __vmaxu4(w.x, w.y);
-                }
-              } else {
+              uint32_t top = 0, low = 255;   // the largest byte of the tile; the least of the tokens' largest (of the values)
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                  if (4 * lane + i < there && !((miss >> (lane >> 2)) & 1u))
-                    top = __vmaxu4(top, BL == 4 ? *reinterpret_cast<const uint32_t*>(src + (4 * lane + i) * 4)
-                                                : *reinterpret_cast<const uint16_t*>(src + (4 * lane + i) * 2));
+              for (int i = 0; i < 4; ++i) {
+                const uint32_t w = largest_byte(BL == 4 ? *reinterpret_cast<const uint32_t*>(src + (4 * lane + i) * 4)
+                                                        : *reinterpret_cast<const uint16_t*>(src + (4 * lane + i) * 2));
+                if (!cut || (4 * lane + i < there && !((miss >> (lane >> 2)) & 1u))) {
+                  top = max(top, w);
+                  low = min(low, w);
+                }
               }
-              top = __vmaxu4(top, top >> 16);
-              top = __reduce_max_sync(0xFFFFFFFFu, max(top & 255u, (top >> 8) & 255u));
-              const int c_tile = max(static_cast<int>(top) - 127 - 7, x == 0 ? -100 : kAtMinScale);
-              cs[x] = c_tile;
+              top = __reduce_max_sync(0xFFFFFFFFu, top);
+              int c_own = x == 0 ? max(static_cast<int>(top) - 127 - 7, -100) : attn_value_exponent(top);
+              cs[x] = c_own;
               const uint32_t w = BL == 4 ? *reinterpret_cast<const uint32_t*>(src + ct * 4) : *reinterpret_cast<const uint16_t*>(src + ct * 2);
+              if (x == 1) {
+                uneven = attn_uneven(top, __reduce_min_sync(0xFFFFFFFFu, low));
+                const int less = uneven ? attn_less(c_own, largest_byte(w)) : 0;
+                c_own -= less;
+                info[slot].less[ct] = static_cast<uint8_t>(less);
+              }
 #pragma unroll
               for (int h = 0; h < BL / 2; ++h) {
-                uint32_t f = f16_pow2x2(__byte_perm(w, 0u, h == 0 ? 0x4140 : 0x4342), c_tile + 127);
+                uint32_t f = f16_pow2x2(__byte_perm(w, 0u, h == 0 ? 0x4140 : 0x4342), c_own + 127);
                 // behind the last key (or on a page that is not there) anything may stand: values count as zero
                 if (x == 1 && cut && (ct >= there || ((miss >> (ct >> 4)) & 1u))) f = 0u;
                 uint16_t* at = &factors[READY ? 0 : x][2 * h * kWdTile + (ct & 7) * 16 + (ct >> 3)];
@@ -538,7 +572,7 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
                 at[kWdTile] = static_cast<uint16_t>(f >> 16);
               }
             }
-            if (ct == 0) { info[slot].ck = cs[0]; info[slot].cv = cs[1]; }
+            if (ct == 0) { info[slot].ck = cs[0]; info[slot].cv = cs[1]; info[slot].uneven = uneven; }
             named_barrier_sync(1, 128);
           }
           const uint8_t* codes = base + Cfg::kCodeAt + st * Cfg::kCodeBytes + code_at;
@@ -758,7 +792,7 @@ __global__ void __launch_bounds__(128) attention_widen_kernel(const __grid_const
   const AttnParams& p = wp.a;
   __shared__ int rows[kWdTile];                    // a token's row of the pool, -1: none
   __shared__ uint16_t factors[2][kWdTile * BL];
-  __shared__ uint32_t tops[2][4], lost[4];
+  __shared__ uint32_t tops[2][4], lows[4], lost[4];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int t = blockIdx.x, head = blockIdx.y, seq = blockIdx.z;
   grid_launch_dependents();
@@ -787,27 +821,39 @@ __global__ void __launch_bounds__(128) attention_widen_kernel(const __grid_const
   const uint32_t gone = __ballot_sync(0xFFFFFFFFu, miss);
 #pragma unroll
   for (int x = 0; x < 2; ++x) {
-    uint32_t top = __vmaxu4(w[x], w[x] >> 16);
-    top = __reduce_max_sync(0xFFFFFFFFu, max(top & 255u, (top >> 8) & 255u));
+    const uint32_t top = __reduce_max_sync(0xFFFFFFFFu, largest_byte(w[x]));
     if (lane == 0) tops[x][warp] = top;
   }
+  const uint32_t low = __reduce_min_sync(0xFFFFFFFFu, row >= 0 ? largest_byte(w[1]) : 255u);
+  if (lane == 0) lows[warp] = low;
   if (lane == 0) lost[warp] = (gone & 0xFFFFu ? 1u : 0u) | (gone >> 16 ? 2u : 0u);
   __syncthreads();
+  const int64_t at = (static_cast<int64_t>(seq) * p.kv_heads + head) * wp.max_tiles + t;
   int c[2];
+  bool uneven = false;
 #pragma unroll
   for (int x = 0; x < 2; ++x) {
     const uint32_t top = max(max(tops[x][0], tops[x][1]), max(tops[x][2], tops[x][3]));
-    c[x] = max(static_cast<int>(top) - 127 - 7, x == 0 ? -100 : kAtMinScale);
+    c[x] = x == 0 ? max(static_cast<int>(top) - 127 - 7, -100) : attn_value_exponent(top);
+    int c_own = c[x];
+    if (x == 1) {
+      uneven = attn_uneven(top, min(min(lows[0], lows[1]), min(lows[2], lows[3])));
+      const int less = uneven ? attn_less(c_own, largest_byte(w[x])) : 0;
+      c_own -= less;
+      wp.info[at].less[tid] = static_cast<uint8_t>(less);
+    }
 #pragma unroll
     for (int h = 0; h < BL / 2; ++h) {
-      const uint32_t f = f16_pow2x2(__byte_perm(w[x], 0u, h == 0 ? 0x4140 : 0x4342), c[x] + 127);
+      const uint32_t f = f16_pow2x2(__byte_perm(w[x], 0u, h == 0 ? 0x4140 : 0x4342), c_own + 127);
       *reinterpret_cast<uint32_t*>(&factors[x][tid * BL + 2 * h]) = row >= 0 ? f : 0u;
     }
   }
-  const int64_t at = (static_cast<int64_t>(seq) * p.kv_heads + head) * wp.max_tiles + t;
   if (tid == 0) {
     const uint32_t all = lost[0] | lost[1] << 2 | lost[2] << 4 | lost[3] << 6;
-    wp.info[at] = AttnTileInfo{c[0], c[1], all, 0};
+    wp.info[at].ck = c[0];
+    wp.info[at].cv = c[1];
+    wp.info[at].missing = all;
+    wp.info[at].uneven = uneven;
     if (all != 0) atomicOr(&g_device_error, kErrorIndex);
   }
   __syncthreads();
