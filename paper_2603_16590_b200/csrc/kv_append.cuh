@@ -297,9 +297,11 @@ __global__ void __launch_bounds__(kKvThreads, GC == 8 || GC == 0 ? 3 : 2) kv_app
       mn = fminf(mn, o[i]);
       mx = fmaxf(mx, o[i]);
     }
-    // Without a clip the ratios are 1 and the bounds the block's own: they take a NaN to a number.  No NaN code is ever
-    // stored: in an attention it would reach rows that do not see its token, as 0 times NaN.
+    // Without a clip the ratios are 1 and the bounds the block's own: they take a NaN to a number, to 0 where there is none
+    // in the block.  No NaN code is ever stored: in an attention it would reach rows that do not see its token, as 0 times
+    // NaN; and no scale that is larger than the numbers need: a tile's keys stand in f16 under one exponent there.
     {
+      if (!(mn <= mx)) mn = mx = 0.0f;
       const float lo = clip_lo * mn, hi = clip_hi * mx;
 #pragma unroll
       for (int i = 0; i < 32; ++i) o[i] = fminf(fmaxf(o[i], lo), hi);

@@ -6,6 +6,7 @@ import pytest
 import torch
 
 import kv_reference as R
+from test_gpu_kv_cache import Append
 
 pytestmark = pytest.mark.gpu
 
@@ -88,3 +89,34 @@ def test_all_values_tiny_or_huge(batq, d, rows, exponent, copy_path):
     got, kq, vq = _attend(batq, q, k, v.double() * 2.0 ** exponent, 32)
     want, bound = _reference(q, kq, vq * 2.0 ** -exponent, d ** -0.5)
     _check(got * 2.0 ** -exponent, want, bound)
+
+
+def test_bad_tokens_of_a_prompt_leave_the_others(batq, copy_path):
+    """A NaN and an infinity among a prompt's tokens: rows that do not see them come out as without them.  In the tiles
+    of 128 tokens in front to the bit, in the bad token's own up to roundings."""
+    heads, kv_heads, d, tokens = 8, 2, 64, 640
+    a = Append(batq, tokens, heads, kv_heads, d, 16, rot=d, transform=True, clip=True, seed=12)
+    slots = torch.arange(tokens)
+    table = torch.arange(tokens // 16, dtype=torch.int32, device="cuda")[None].contiguous()
+    starts, lens = torch.tensor([0, tokens], dtype=torch.int32, device="cuda"), torch.tensor([tokens], dtype=torch.int32, device="cuda")
+    x = a.x.cuda()
+    bad = x.clone()
+    bad[300, heads * d + 3] = math.nan                                      # a key
+    bad[300, (heads + kv_heads) * d:(heads + kv_heads) * d + 32] = math.nan  # a block of values
+    bad[560, heads * d + 70] = math.inf
+    bad[560, (heads + kv_heads) * d + 1] = -math.inf
+    outs = []
+    for y in (x, bad):
+        q_out = torch.empty(tokens, heads * d, dtype=torch.bfloat16, device="cuda")
+        a.run(batq, x=y, q_out=q_out, slots=slots)
+        out = torch.zeros_like(q_out)
+        ws = batq.aligned_workspace(batq.batq_attention_kv_mxfp8_workspace_bytes(a.cache, heads, tokens, 1, tokens, tokens))
+        batq.batq_attention_kv_mxfp8(a.cache, q_out, out, lens, table, tokens, tokens, ws, q_starts=starts)
+        assert batq.batq_last_device_status() == 0
+        outs.append(out.float())
+        if y is x:
+            clean = [a.pool[2].clone(), a.pool[3].clone()]
+    assert torch.equal(outs[0][:256], outs[1][:256])
+    # weights are off by 2^-11 of themselves on both sides, their scores are the same
+    most = R.values(*[b.cpu() for b in clean]).abs().max()
+    assert ((outs[0] - outs[1])[256:300].abs().cpu() <= outs[0][256:300].abs().cpu() * 2.0 ** -7 + most * 2.0 ** -9).all()
