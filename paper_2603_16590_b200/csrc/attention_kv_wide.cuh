@@ -169,6 +169,7 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
   __shared__ __align__(16) uint16_t factors[READY ? 1 : 2][READY ? 1 : kWdTile * BL];
   __shared__ uint32_t tmem_base_smem;
   __shared__ int abort_flag;
+  __shared__ volatile int widen_stop;   // a widening warp's wait has run out
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(wd_smem) + 1023) & ~uintptr_t(1023));
 
@@ -189,6 +190,7 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
     mbar_init(smem_u32(&drain), 1);
     mbar_fence_init();
     abort_flag = 0;
+    widen_stop = 0;
     if (!READY) {
       tma_prefetch_desc(&tmap_k);
       tma_prefetch_desc(&tmap_v);
@@ -530,15 +532,19 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
 #pragma unroll
         for (int v = 0; v < 2; ++v, ++n_step) {   // K, then V
           const uint32_t st = n_step % kStages, phase = (n_step / kStages) & 1u;
-          ok = __all_sync(0xFFFFFFFFu, mbar_wait_short(smem_u32(&code_full[st]), phase, &abort_flag) &&
-                                           mbar_wait_short(smem_u32(&f16_empty[st]), phase ^ 1u, &abort_flag));
-          if (!ok) break;
+          const bool got = __all_sync(0xFFFFFFFFu, mbar_wait_short(smem_u32(&code_full[st]), phase, &abort_flag) &&
+                                                       mbar_wait_short(smem_u32(&f16_empty[st]), phase ^ 1u, &abort_flag));
+          // The four warps leave together: one that went by its own wait would be missed at the barriers below, whose
+          // waits have no limit.  The flag is written in front of the first or behind the second, and read in between.
+          if (!got && lane == 0) widen_stop = 1;
           if (v == 0) {
+            // (the tile before is widened everywhere: its factors go)
+            named_barrier_sync(1, 128);
+            ok = widen_stop == 0;
+            if (!ok) break;
             // the tile's exponents, in every warp (a lane has four tokens), then the factors of the thread's own token
             miss = info[slot].missing;
             cut = there < kWdTile || miss != 0;
-            // (the tile before is widened everywhere: its factors go)
-            named_barrier_sync(1, 128);
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
               const uint8_t* src = x == 0 ? ks : vs;
@@ -575,6 +581,7 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
             if (ct == 0) { info[slot].ck = cs[0]; info[slot].cv = cs[1]; info[slot].uneven = uneven; }
             named_barrier_sync(1, 128);
           }
+          if (!got) continue;   // (the values': on to the next tile's first barrier, if there is one)
           const uint8_t* codes = base + Cfg::kCodeAt + st * Cfg::kCodeBytes + code_at;
           uint8_t* dst = base + Cfg::kF16At + st * Cfg::kF16Bytes + f16_at;
           const uint4 fs = *reinterpret_cast<const uint4*>(&factors[READY ? 0 : v][b * kWdTile + (r0 & 7) * 16 + half * 8]);
