@@ -643,11 +643,10 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
           }
         }
       }
-      if (!ok) {   // given up: copies already in flight land before the CTA leaves
-        for (uint32_t i = n_step > kStages ? n_step - kStages : 0; i < n_step; ++i) {
-          const uint64_t t0 = global_timer_ns();
-          while (!mbar_try_wait(smem_u32(&f16_full[i % kStages]), (i / kStages) & 1u) && global_timer_ns() - t0 < 100000000ull) {}
-        }
+      // copies in flight land before the CTA leaves: whoever waits for the last ones may have given up
+      for (uint32_t i = n_step > kStages ? n_step - kStages : 0; i < n_step; ++i) {
+        const uint64_t t0 = global_timer_ns();
+        while (!mbar_try_wait(smem_u32(&f16_full[i % kStages]), (i / kStages) & 1u) && global_timer_ns() - t0 < 100000000ull) {}
       }
     } else if (!READY && warp == Shape::kIssueWarp) {
       // ---------------------------------------------------------------- codes and scales by TMA
@@ -703,11 +702,10 @@ attention_kv_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __gri
           }
         }
       }
-      if (!ok) {   // given up: copies already in flight land before the CTA leaves
-        for (uint32_t i = n_step > kStages ? n_step - kStages : 0; i < n_step; ++i) {
-          const uint64_t t0 = global_timer_ns();
-          while (!mbar_try_wait(smem_u32(&code_full[i % kStages]), (i / kStages) & 1u) && global_timer_ns() - t0 < 100000000ull) {}
-        }
+      // copies in flight land before the CTA leaves: whoever waits for the last ones may have given up
+      for (uint32_t i = n_step > kStages ? n_step - kStages : 0; i < n_step; ++i) {
+        const uint64_t t0 = global_timer_ns();
+        while (!mbar_try_wait(smem_u32(&code_full[i % kStages]), (i / kStages) & 1u) && global_timer_ns() - t0 < 100000000ull) {}
       }
     } else if (warp == Shape::kIssueWarp + 1) {
       // ---------------------------------------------------------------- MMAs
