@@ -309,7 +309,8 @@ batq_status batq_kv_cache_create(batq_kv_cache** out, void* k_codes, void* k_sca
                                  int64_t pages, int32_t page_size, int32_t kv_heads, int32_t head_dim);
 batq_status batq_kv_cache_destroy(batq_kv_cache* c);
 
-/* New tokens into the cache, and their queries through the same rotation, in one launch.  With x = (x_1, x_2) the
+/* New tokens into the cache, and their queries through the same rotation, in one launch (one for each size of factors,
+ * where these differ).  With x = (x_1, x_2) the
  * halves of the first rot_dim channels of a head and (cos, sin) its token's row of the table,
  *   rope(x) = (x_1 cos - x_2 sin, x_2 cos + x_1 sin, the other channels as they are);
  *   keys     MXFP8(clip(rope(k) P_k)),  values  MXFP8(clip(v P_v))   to the token's slot,
@@ -322,8 +323,9 @@ batq_status batq_kv_cache_destroy(batq_kv_cache* c);
  *   k, v           dev bf16 [tokens x kv_heads * head_dim], row strides ldk, ldv elements: e.g. column ranges of the
  *                  output of the qkv projection.
  *   slots          dev int64 [tokens]: where each token goes.  A negative slot marks a padding row: nothing of it is
- *                  read or written, its row of q_out is left as it was.  The others must differ from one another (a
- *                  slot given twice holds a mixture of the two tokens).
+ *                  written, its row of q_out is left as it was.  Its rows of k, v, q and its position have to be there
+ *                  (they are fetched beside the slot), and may hold anything.  The other slots must differ from one
+ *                  another (a slot given twice holds a mixture of the two tokens).
  *   positions      dev int32 [tokens]: the token's row of the table; NULL: row i for token i (a table gathered per
  *                  token, as a rotation with several position components needs it).
  *   rope           dev fp32 [rope_rows x rot_dim], rot_dim / 2 cosines then rot_dim / 2 sines per row, 16-byte
