@@ -355,14 +355,18 @@ batq_status batq_kv_append_mxfp8(const batq_kv_cache* c, const batq_transform* t
  *   page_table   dev int32 [seqs x ld_pages]: the pages of each sequence in the order of its tokens.  Entries behind
  *                a sequence's last page are not read.  A page outside the pool: its keys are left out and the next
  *                batq_last_device_status returns BATQ_ERR_INDEX.
- *   max_q        no sequence has more query rows; max_kv (<= 2^30): none has more keys.  Bounds that size the grid and the
+ *   max_q        no sequence has more query rows; max_kv: none has more keys.  Bounds that size the grid and the
  *                workspace (a captured call is replayed with other lengths within them); what a sequence has beyond
- *                them, or beyond ld_pages * page_size keys, is not looked at.
+ *                them, or beyond ld_pages * page_size keys, is not looked at.  SHAPE where they count past 32 bits: max_kv
+ *                above 2^30, or above 2^28 - 128 where a sequence may have more than 48 rows (max_q x heads of a group);
+ *                2^31 tiles of 32 keys over sequences (up to 512), key/value heads and units of 8 rows and more, each
+ *                unit counting 12 tiles besides its own (e.g. 512 sequences x 8 heads x 16.7 million keys); 2^21 units of 256 rows.
  *   lse          dev fp32 [tokens x q_heads] or NULL.
- *   workspace    dev, batq_attention_kv_mxfp8_workspace_bytes(...) bytes with the same sizes (may be 0), 256-byte
- *                aligned; contents need not be initialised; calls sharing it must be ordered on one stream.  A few MB
+ *   workspace    dev, batq_attention_kv_mxfp8_workspace_bytes(...) bytes with the same sizes (0: none is wanted,
+ *                or the call would be refused), 256-byte aligned; contents need not be initialised; calls sharing it must be ordered on one stream.  A few MB
  *                for decoding, up to 40 MB for prompts; where prompts pay for it, also an f16 copy of the keys and values,
- *                seqs * max_kv * kv_heads * head_dim * 4 bytes, at most 512 MB.
+ *                seqs * max_kv * kv_heads * head_dim * 4 bytes, at most 512 MB.  Smaller sizes may want more than larger
+ *                ones (a copy that would pass 512 MB is left out): one workspace for several has the largest of their bytes.
  * Repeated, a call gives the same bits: nothing depends on the order in which parts finish.  The last bits of a row may
  * depend on the lengths of the other sequences, which move the places where long sequences are divided.
  * Finite q, keys and values.  Scores and sums are fp32.  Softmax weights are f16: off by 2^-11 of themselves, or by
