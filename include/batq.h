@@ -361,6 +361,7 @@ batq_status batq_kv_append_mxfp8(const batq_kv_cache* c, const batq_transform* t
  *                above 2^30, or above 2^28 - 128 where a sequence may have more than 48 rows (max_q x heads of a group);
  *                2^31 tiles of 32 keys over sequences (up to 512), key/value heads and units of 8 rows and more, each
  *                unit counting 12 tiles besides its own (e.g. 512 sequences x 8 heads x 16.7 million keys); 2^21 units of 256 rows.
+ *   scale        |scale| < 2.35e38 (scale * log2(e) is finite; else SHAPE).
  *   lse          dev fp32 [tokens x q_heads] or NULL.
  *   workspace    dev, batq_attention_kv_mxfp8_workspace_bytes(...) bytes with the same sizes (0: none is wanted,
  *                or the call would be refused), 256-byte aligned; contents need not be initialised; calls sharing it must be ordered on one stream.  A few MB

@@ -2807,8 +2807,10 @@ batq_status batq_attention_kv_mxfp8(const batq_kv_cache* c, const void* q_bf16, 
                                     void* stream) {
   if (c == nullptr) return BATQ_ERR_NULL;
   if (q_heads <= 0 || q_heads % c->kv_heads != 0 || q_heads > kKvMaxHeads || tokens < 0 || tokens > (int64_t(1) << 30) || seqs < 0 ||
-      max_q <= 0 || max_kv < 0 || max_kv > (1 << 30) || ld_pages < 0 || !std::isfinite(scale))
+      max_q <= 0 || max_kv < 0 || max_kv > (1 << 30) || ld_pages < 0)
     return BATQ_ERR_SHAPE;
+  const float scale_log2 = static_cast<float>(static_cast<double>(scale) * 1.4426950408889634);   // times a score of 0 it has to be 0
+  if (!std::isfinite(scale_log2)) return BATQ_ERR_SHAPE;
   if (q_starts == nullptr && tokens != seqs) return BATQ_ERR_SHAPE;
   if (seqs == 0 || tokens == 0) return BATQ_OK;
   if (kv_lens == nullptr || (page_table == nullptr && ld_pages > 0)) return BATQ_ERR_NULL;
@@ -2841,7 +2843,7 @@ batq_status batq_attention_kv_mxfp8(const batq_kv_cache* c, const void* q_bf16, 
   p.pages = static_cast<int32_t>(c->pages);
   p.k_scales = c->k_scales;
   p.v_scales = c->v_scales;
-  p.scale_log2 = static_cast<float>(static_cast<double>(scale) * 1.4426950408889634);
+  p.scale_log2 = scale_log2;
   p.causal = causal != 0;
   p.out = static_cast<uint16_t*>(out_bf16);
   p.ldo = ldo;

@@ -53,3 +53,11 @@ def test_bounds_past_the_limits(lib, sizes):
     c, bytes_of, attend = _calls(lib)
     assert bytes_of(*sizes) == 0
     assert attend(*sizes) == SHAPE
+
+
+@pytest.mark.parametrize("scale", [math.nan, math.inf, -math.inf, 3e38, -2.4e38])
+def test_scales_that_are_infinite_in_base_two(lib, scale):
+    """The kernels work with scale * log2(e) in fp32: an infinite one would make 0 * infinity of a score of 0."""
+    c, _, attend = _calls(lib)
+    assert attend(32, 1, 1, 1, 100000, scale=scale) == SHAPE
+    assert attend(32, 1, 1, 1, 100000, scale=2.3e38) == 1
