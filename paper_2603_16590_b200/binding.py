@@ -437,11 +437,13 @@ class KVCache:
             if x.dtype != torch.uint8 or not x.is_contiguous() or tuple(x.shape) != (pages, heads, page_size, last):
                 raise ValueError("batq_kv_cache_create: dense uint8 buffers, codes [pages, kv_heads, page_size, head_dim] and "
                                  "scales [pages, kv_heads, page_size, head_dim / 32]")
+            if not x.is_cuda or x.get_device() != k_codes.get_device():
+                raise ValueError("batq_kv_cache_create: buffers of one CUDA device")
         h = _P()
         _check(load().batq_kv_cache_create(C.byref(h), _ptr(k_codes), _ptr(k_scales), _ptr(v_codes), _ptr(v_scales), pages, page_size,
                                            heads, d), "batq_kv_cache_create")
         self.k_codes, self.k_scales, self.v_codes, self.v_scales = k_codes, k_scales, v_codes, v_scales
-        self.handle, self.kv_heads, self.head_dim = h, heads, d
+        self.handle, self.kv_heads, self.head_dim, self.device_index = h, heads, d, k_codes.get_device()
 
     def close(self):
         if self.handle:
@@ -458,6 +460,13 @@ class KVCache:
 def batq_kv_cache_create(k_codes, k_scales, v_codes, v_scales) -> KVCache:
     """uint8 CUDA buffers: codes [pages, kv_heads, page_size, head_dim], scales [pages, kv_heads, page_size, head_dim / 32]."""
     return KVCache(k_codes, k_scales, v_codes, v_scales)
+
+
+def _on(device, **tensors):
+    """The kernels would not find the host's memory, nor another GPU's."""
+    for what, x in tensors.items():
+        if x is not None and x.get_device() != device:
+            raise ValueError(f"{what}: on device {x.get_device()}, the cache is on {device}")
 
 
 def _vector(x, dtype, n, what):
@@ -477,10 +486,12 @@ def batq_kv_append_mxfp8(cache: KVCache, t_k, t_v, k, v, slots, positions=None, 
     [rows, rot_dim], cosines then sines."""
     if _LIB is None:
         load()
+    device = getattr(cache, "device_index", -1)
     if _CALL is not None:
-        st = _CALL.kv_append(_ADDRESS["batq_kv_append_mxfp8"], _handle(cache), cache.kv_heads, cache.head_dim, _handle(t_k), _handle(t_v),
+        st = _CALL.kv_append(_ADDRESS["batq_kv_append_mxfp8"], _handle(cache), device, cache.kv_heads, cache.head_dim, _handle(t_k), _handle(t_v),
                              _handle(t_q), k, v, q, q_out, slots, positions, rope, _stream())
     else:
+        _on(device, k=k, v=v, slots=slots, positions=positions, rope=rope, q=q, q_out=q_out)
         tokens, width = k.size(0), cache.kv_heads * cache.head_dim
         _rows(k, tokens, width, "k")
         _rows(v, tokens, width, "v")
@@ -513,10 +524,12 @@ def batq_attention_kv_mxfp8(cache: KVCache, q, out, kv_lens, page_table, max_q, 
     if _LIB is None:
         load()
     scale = cache.head_dim ** -0.5 if scale is None else scale
+    device = getattr(cache, "device_index", -1)
     if _CALL is not None:
-        st = _CALL.attention(_ADDRESS["batq_attention_kv_mxfp8"], _handle(cache), cache.head_dim, q, out, kv_lens, page_table, max_q, max_kv,
+        st = _CALL.attention(_ADDRESS["batq_attention_kv_mxfp8"], _handle(cache), device, cache.head_dim, q, out, kv_lens, page_table, max_q, max_kv,
                              workspace, q_starts, scale, 1 if causal else 0, lse, _stream())
     else:
+        _on(device, q=q, out=out, kv_lens=kv_lens, page_table=page_table, workspace=workspace, q_starts=q_starts, lse=lse)
         tokens, seqs = q.size(0), kv_lens.size(0)
         _rows(q, tokens, 0, "q")
         _rows(out, tokens, q.size(1), "out")

@@ -6,7 +6,7 @@
 #include <Python.h>
 #include <stdint.h>
 
-static PyObject *s_data_ptr, *s_size, *s_shape, *s_stride, *s_numel, *s_is_contiguous, *s_dtype, *zero, *one, *float32_type, *bfloat16_type, *int32_type, *int64_type;
+static PyObject *s_data_ptr, *s_size, *s_shape, *s_stride, *s_numel, *s_is_contiguous, *s_dtype, *s_get_device, *zero, *one, *float32_type, *bfloat16_type, *int32_type, *int64_type;
 static PyTypeObject *tensor_type;
 
 typedef int (*linear_fn)(const void *, const void *, const void *, int64_t, int64_t, void *, int32_t, int64_t, void *, size_t,
@@ -101,8 +101,16 @@ static int as_int32(PyObject *o, int32_t *out) {
   return 0;
 }
 
-/* The kernels take sizes and types on trust: a tensor that is shorter, or of another type, would be read or written
- * past its end.  So these two look at what they are given (as binding.py does where this shim is missing). */
+/* The kernels take sizes, types and places on trust: a tensor that is shorter, or of another type, would be read or written
+ * past its end, one of the host's or of another GPU's memory is not there for them.  So these two look at what they are
+ * given (as binding.py does where this shim is missing); for the devices that is 0.5 us a call. */
+static int is_on(PyObject *o, int64_t device, const char *what) {
+  int64_t at;
+  if (as_int(o, s_get_device, NULL, &at)) return -1;
+  if (at != device) { PyErr_Format(PyExc_ValueError, "%s: on device %lld, the cache is on %lld", what, (long long)at, (long long)device); return -1; }
+  return 0;
+}
+
 static int is_type(PyObject *o, PyObject *want, const char *what) {
   PyObject *dt = PyObject_GetAttr(o, s_dtype);
   if (dt == NULL) return -1;
@@ -112,10 +120,10 @@ static int is_type(PyObject *o, PyObject *want, const char *what) {
 }
 
 /* A bf16 matrix of at least `tokens` rows and, unless 0, of `width` columns, which are dense: address, rows, columns, stride. */
-static int as_rows(PyObject *o, int64_t tokens, int64_t width, const char *what, void **p, int64_t *n, int64_t *w, int64_t *ld) {
+static int as_rows(PyObject *o, int64_t device, int64_t tokens, int64_t width, const char *what, void **p, int64_t *n, int64_t *w, int64_t *ld) {
   int64_t step;
   if (is_type(o, bfloat16_type, what) || as_pointer(o, p) || as_extent(o, zero, n) || as_extent(o, one, w) || as_int(o, s_stride, zero, ld) ||
-      as_int(o, s_stride, one, &step))
+      as_int(o, s_stride, one, &step) || is_on(o, device, what))
     return -1;
   if (*n < tokens || (width != 0 && *w != width) || *w == 0 || (step != 1 && *w > 1)) {
     PyErr_Format(PyExc_ValueError, "%s: %lld dense bf16 rows, %lld wide", what, (long long)tokens, (long long)(width ? width : *w));
@@ -125,32 +133,32 @@ static int as_rows(PyObject *o, int64_t tokens, int64_t width, const char *what,
 }
 
 /* A dense vector of at least n entries, or None. */
-static int as_vector(PyObject *o, PyObject *type, int64_t n, const char *what, void **p) {
+static int as_vector(PyObject *o, int64_t device, PyObject *type, int64_t n, const char *what, void **p) {
   if (as_pointer(o, p) || o == Py_None) return PyErr_Occurred() ? -1 : 0;
   int64_t size, step;
-  if (is_type(o, type, what) || as_extent(o, zero, &size) || as_int(o, s_stride, zero, &step)) return -1;
+  if (is_type(o, type, what) || as_extent(o, zero, &size) || as_int(o, s_stride, zero, &step) || is_on(o, device, what)) return -1;
   if (size < n || (step != 1 && n > 1)) { PyErr_Format(PyExc_ValueError, "%s: a dense vector of %lld entries", what, (long long)n); return -1; }
   return 0;
 }
 
-/* kv_append(function, cache, kv_heads, head_dim, t_k, t_v, t_q, k, v, q, q_out, slots, positions, rope, stream) -> status */
+/* kv_append(function, cache, device, kv_heads, head_dim, t_k, t_v, t_q, k, v, q, q_out, slots, positions, rope, stream) -> status */
 static PyObject *kv_append(PyObject *self, PyObject *const *a, Py_ssize_t n) {
   (void)self;
-  if (n != 15) { PyErr_SetString(PyExc_TypeError, "kv_append: 15 arguments"); return NULL; }
+  if (n != 16) { PyErr_SetString(PyExc_TypeError, "kv_append: 16 arguments"); return NULL; }
   void *fn, *c, *tk, *tv, *tq, *k, *v, *q = NULL, *q_out = NULL, *slots, *positions, *rope, *stream;
   int64_t ldk, ldv, ldq = 0, ldqo = 0, tokens, rows, w, width = 0, rope_rows = 0, rot = 0, step;
-  int32_t heads, d;
-  if (as_pointer(a[0], &fn) || as_pointer(a[1], &c) || as_int32(a[2], &heads) || as_int32(a[3], &d) || as_pointer(a[4], &tk) ||
-      as_pointer(a[5], &tv) || as_pointer(a[6], &tq) || as_rows(a[7], 0, (int64_t)heads * d, "k", &k, &tokens, &w, &ldk) ||
-      as_rows(a[8], tokens, (int64_t)heads * d, "v", &v, &rows, &w, &ldv) || as_vector(a[11], int64_type, tokens, "slots", &slots) ||
-      as_vector(a[12], int32_type, tokens, "positions", &positions) || as_pointer(a[13], &rope) || as_pointer(a[14], &stream))
+  int32_t heads, d, dev;
+  if (as_pointer(a[0], &fn) || as_pointer(a[1], &c) || as_int32(a[2], &dev) || as_int32(a[3], &heads) || as_int32(a[4], &d) || as_pointer(a[5], &tk) ||
+      as_pointer(a[6], &tv) || as_pointer(a[7], &tq) || as_rows(a[8], dev, 0, (int64_t)heads * d, "k", &k, &tokens, &w, &ldk) ||
+      as_rows(a[9], dev, tokens, (int64_t)heads * d, "v", &v, &rows, &w, &ldv) || as_vector(a[12], dev, int64_type, tokens, "slots", &slots) ||
+      as_vector(a[13], dev, int32_type, tokens, "positions", &positions) || as_pointer(a[14], &rope) || as_pointer(a[15], &stream))
     return NULL;
-  if (a[9] != Py_None && as_rows(a[9], tokens, 0, "q", &q, &rows, &width, &ldq)) return NULL;
+  if (a[10] != Py_None && as_rows(a[10], dev, tokens, 0, "q", &q, &rows, &width, &ldq)) return NULL;
   if (width % d != 0) { PyErr_SetString(PyExc_ValueError, "q: whole heads"); return NULL; }
-  if (a[10] != Py_None && as_rows(a[10], tokens, width, "q_out", &q_out, &rows, &w, &ldqo)) return NULL;
-  if (a[13] != Py_None) {
-    if (is_type(a[13], float32_type, "rope") || as_extent(a[13], zero, &rope_rows) || as_extent(a[13], one, &rot) || as_int(a[13], s_stride, zero, &w) ||
-        as_int(a[13], s_stride, one, &step))
+  if (a[11] != Py_None && as_rows(a[11], dev, tokens, width, "q_out", &q_out, &rows, &w, &ldqo)) return NULL;
+  if (a[14] != Py_None) {
+    if (is_type(a[14], float32_type, "rope") || as_extent(a[14], zero, &rope_rows) || as_extent(a[14], one, &rot) || as_int(a[14], s_stride, zero, &w) ||
+        as_int(a[14], s_stride, one, &step) || is_on(a[14], dev, "rope"))
       return NULL;
     if (step != 1 || (w != rot && rope_rows > 1)) { PyErr_SetString(PyExc_ValueError, "rope: a dense float32 table"); return NULL; }
   }
@@ -162,37 +170,37 @@ static PyObject *kv_append(PyObject *self, PyObject *const *a, Py_ssize_t n) {
   return PyLong_FromLong(st);
 }
 
-/* attention(function, cache, head_dim, q, out, kv_lens, page_table, max_q, max_kv, workspace, q_starts, scale, causal, lse,
+/* attention(function, cache, device, head_dim, q, out, kv_lens, page_table, max_q, max_kv, workspace, q_starts, scale, causal, lse,
  * stream) -> status */
 static PyObject *attention(PyObject *self, PyObject *const *a, Py_ssize_t n) {
   (void)self;
-  if (n != 15) { PyErr_SetString(PyExc_TypeError, "attention: 15 arguments"); return NULL; }
+  if (n != 16) { PyErr_SetString(PyExc_TypeError, "attention: 16 arguments"); return NULL; }
   void *fn, *c, *q, *out, *lens, *table, *ws, *starts, *lse, *stream;
   int64_t ldq, width, tokens, ldo, seqs, table_rows, ld_pages, step, rows, w, bytes = 0, size;
-  int32_t max_q, max_kv, causal, d;
-  if (as_pointer(a[0], &fn) || as_pointer(a[1], &c) || as_int32(a[2], &d) || as_rows(a[3], 0, 0, "q", &q, &tokens, &width, &ldq) ||
-      as_rows(a[4], tokens, width, "out", &out, &rows, &w, &ldo) || as_extent(a[5], zero, &seqs) ||
-      as_vector(a[5], int32_type, seqs, "kv_lens", &lens) || is_type(a[6], int32_type, "page_table") || as_pointer(a[6], &table) ||
-      as_extent(a[6], zero, &table_rows) || as_extent(a[6], one, &ld_pages) || as_int(a[6], s_stride, zero, &w) ||
-      as_int(a[6], s_stride, one, &step) || as_int32(a[7], &max_q) || as_int32(a[8], &max_kv) || as_pointer(a[9], &ws) ||
-      as_vector(a[10], int32_type, seqs + 1, "q_starts", &starts) || as_int32(a[12], &causal) || as_pointer(a[13], &lse) ||
-      as_pointer(a[14], &stream))
+  int32_t max_q, max_kv, causal, d, dev;
+  if (as_pointer(a[0], &fn) || as_pointer(a[1], &c) || as_int32(a[2], &dev) || as_int32(a[3], &d) || as_rows(a[4], dev, 0, 0, "q", &q, &tokens, &width, &ldq) ||
+      as_rows(a[5], dev, tokens, width, "out", &out, &rows, &w, &ldo) || as_extent(a[6], zero, &seqs) ||
+      as_vector(a[6], dev, int32_type, seqs, "kv_lens", &lens) || is_type(a[7], int32_type, "page_table") || is_on(a[7], dev, "page_table") || as_pointer(a[7], &table) ||
+      as_extent(a[7], zero, &table_rows) || as_extent(a[7], one, &ld_pages) || as_int(a[7], s_stride, zero, &w) ||
+      as_int(a[7], s_stride, one, &step) || as_int32(a[8], &max_q) || as_int32(a[9], &max_kv) || as_pointer(a[10], &ws) ||
+      as_vector(a[11], dev, int32_type, seqs + 1, "q_starts", &starts) || as_int32(a[13], &causal) || as_pointer(a[14], &lse) ||
+      as_pointer(a[15], &stream))
     return NULL;
   if (table_rows < seqs || (step != 1 && ld_pages > 1) || (w != ld_pages && table_rows > 1)) {
     PyErr_SetString(PyExc_ValueError, "page_table: dense int32, a row per sequence");
     return NULL;
   }
   if (width % d != 0) { PyErr_SetString(PyExc_ValueError, "q: whole heads"); return NULL; }
-  if (a[13] != Py_None) {
-    PyObject *dense = PyObject_CallMethodNoArgs(a[13], s_is_contiguous);
+  if (a[14] != Py_None) {
+    PyObject *dense = PyObject_CallMethodNoArgs(a[14], s_is_contiguous);
     if (dense == NULL) return NULL;
     const int yes = PyObject_IsTrue(dense);
     Py_DECREF(dense);
-    if (yes < 0 || is_type(a[13], float32_type, "lse") || as_int(a[13], s_numel, NULL, &size)) return NULL;
+    if (yes < 0 || is_type(a[14], float32_type, "lse") || is_on(a[14], dev, "lse") || as_int(a[14], s_numel, NULL, &size)) return NULL;
     if (!yes || size < tokens * (width / d)) { PyErr_SetString(PyExc_ValueError, "lse: dense float32, [tokens, q_heads]"); return NULL; }
   }
-  if (a[9] != Py_None && as_int(a[9], s_numel, NULL, &bytes)) return NULL;
-  const double scale = PyFloat_AsDouble(a[11]);
+  if (a[10] != Py_None && (as_int(a[10], s_numel, NULL, &bytes) || is_on(a[10], dev, "workspace"))) return NULL;
+  const double scale = PyFloat_AsDouble(a[12]);
   if (scale == -1.0 && PyErr_Occurred()) return NULL;
   int st;
   Py_BEGIN_ALLOW_THREADS
@@ -230,8 +238,9 @@ PyMODINIT_FUNC PyInit__pycall(void) {
   s_numel = PyUnicode_InternFromString("numel");
   s_is_contiguous = PyUnicode_InternFromString("is_contiguous");
   s_dtype = PyUnicode_InternFromString("dtype");
+  s_get_device = PyUnicode_InternFromString("get_device");
   zero = PyLong_FromLong(0);
   one = PyLong_FromLong(1);
-  if (!s_data_ptr || !s_size || !s_shape || !s_stride || !s_numel || !s_is_contiguous || !s_dtype || !zero || !one) return NULL;
+  if (!s_data_ptr || !s_size || !s_shape || !s_stride || !s_numel || !s_is_contiguous || !s_dtype || !s_get_device || !zero || !one) return NULL;
   return PyModule_Create(&module);
 }
