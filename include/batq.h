@@ -80,7 +80,7 @@ batq_status batq_transform_destroy(batq_transform* t);
 /* The dual P^-T = diag(P_1^-T..P_k^-T) of a transform, without clip: what the queries go through where the
  * keys go through P, so that (q P^-T)(k P)^T = q k^T (Sec. 3.2's head-by-head key transform).  The factors'
  * inverses are computed in fp64 and rounded to fp32.  A handle of its own, on t's device, which must be
- * current; destroyed with batq_transform_destroy.  SINGULAR if a factor has no inverse. */
+ * current; destroyed with batq_transform_destroy.  SINGULAR if a factor has no inverse that fp32 holds. */
 batq_status batq_transform_create_dual(batq_transform** out, const batq_transform* t);
 
 /* Emulation of a BF16 implementation of the transform (Sec. 3.2 keeps the pre-quantization

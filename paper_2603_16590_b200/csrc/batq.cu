@@ -338,14 +338,18 @@ bool invert_small(const double* a, int n, double* inv) {
   return true;
 }
 
-// The transposed inverses of `count / (n * n)` matrices, rounded to fp32; false where one has none.
+// The transposed inverses of `count / (n * n)` matrices, rounded to fp32; false where one has none that fp32 holds.
 bool inverse_transposed(const float* a, size_t count, int n, float* out) {
   std::vector<double> m(static_cast<size_t>(n) * n), inv(m.size());
   for (size_t at = 0; at < count; at += m.size()) {
     for (size_t i = 0; i < m.size(); ++i) m[i] = a[at + i];
     if (!invert_small(m.data(), n, inv.data())) return false;
     for (int r = 0; r < n; ++r)
-      for (int c = 0; c < n; ++c) out[at + static_cast<size_t>(r) * n + c] = static_cast<float>(inv[static_cast<size_t>(c) * n + r]);
+      for (int c = 0; c < n; ++c) {
+        const float v = static_cast<float>(inv[static_cast<size_t>(c) * n + r]);
+        if (!std::isfinite(v)) return false;
+        out[at + static_cast<size_t>(r) * n + c] = v;
+      }
   }
   return true;
 }

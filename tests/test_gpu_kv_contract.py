@@ -4,6 +4,7 @@ import math
 import pytest
 import torch
 
+from paper_2603_16590_b200 import synth
 from test_gpu_kv_cache import Append
 
 pytestmark = pytest.mark.gpu
@@ -21,3 +22,14 @@ def test_padding_rows_may_hold_anything(batq, tokens, d):
     a.run(batq, x=x, positions=positions)
     assert batq.batq_last_device_status() == 0
     a.check()
+
+
+def test_dual_that_fp32_does_not_hold(batq):
+    """Factors whose inverses pass fp32: refused as singular, no infinity goes into the queries."""
+    t = synth.make_transform(128, 3, "paper")
+    for left, right in ((t.left * 1e-39, t.right), (t.left, t.right * 1e-40)):
+        small = batq.batq_transform_create(128, left, right)
+        with pytest.raises(batq.BatqError) as e:
+            batq.batq_transform_create_dual(small)
+        assert e.value.status == 6
+    assert batq.batq_transform_create_dual(batq.batq_transform_create(128, t.left * 1e-30, t.right * 1e-30)).n == 128
