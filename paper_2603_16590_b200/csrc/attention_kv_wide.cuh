@@ -7,28 +7,32 @@
 //
 //   tensor memory  S0 | S1 | O0 | O1, 128 columns each; the weights P (f16, two per column) overwrite their S and are the
 //                  A operand of the value product from there.
-//   warps 0-7      softmax: a thread owns a row.  While one M tile's warps are in their exponentials, the tensor cores are
+//   warps 0-7      softmax: a thread owns a row.  While one M tile's warps are in their exponentials, the tensor cores can be
 //                  at the other's products.  The reference follows the maximum only beyond 2^8 (as in attention_kv.cuh),
 //                  so O is hardly ever read back before the end.
 //   the others     one warp brings tiles, one issues the MMAs, and without READY four widen the codes: K 2^(ek - ck) and
 //                  V 2^(ev - cv) in f16, ck and cv one integer per 128 tokens, into 128-byte-swizzled tiles (K: K-major B
 //                  operand; V: MN-major B operand, the same bytes).  Where a token's values are more than 2^kWdEven
-//                  smaller than the tile's largest, each token has its own cv, as in attention_kv.cuh: its weights
-//                  would else count against the reference with the size of its neighbours' values.  The block-scaled kinds would take the codes as they
-//                  are, but want q and P in 8 bits, and V's scales along the wrong axis.
+//                  smaller than the tile's largest, each token has its own cv, as in attention_kv.cuh: its weight
+//                  would else count against the reference with the size of its neighbours' values.  Such a tile's softmax
+//                  takes longer (a prompt of 8192 with nothing but such tiles 790 us instead of 500); the first one of
+//                  a prompt often is one, hardly any other.  The block-scaled kinds would take the codes as they are, but want q
+//                  and P in 8 bits, and V's scales along the wrong axis.
 //
-// What bounds it is instruction issue beside the exponentials: on each of an SM's four schedulers two softmax warps (some
-// 450 instructions a tile each; 128 exponentials of 8 cycles) take 2260 cycles a tile by themselves, and the four widening
-// warps, 250 instructions a tile, double that (measured in isolation).  So where a sequence and head has several units
-// and many tiles, attention_widen_kernel writes the f16 tiles to the workspace once and this kernel copies them (READY): a prompt
-// of 8192 tokens, 28 / 4 heads, takes 490 us (0.98 PFLOP/s, 0.6 of what a large bf16 product reaches) against 742, one of
-// 2048, 32 / 8 heads, 71 against 82.  A tile pair then takes some 3900 cycles: 2200 of softmax, 1100 of products, the rest
-// waits and issue.  An item's end and the next one's start cost some 15000.
+// What bounds it is that exponentials and products wait for one another: 256 rows x 128 tokens take 2048 cycles of the XU
+// pipes (2260 as a softmax by itself) and 2048 of the tensor cores (32 MMAs of 64), and come to some 3900.  Scores ->
+// weights -> P V -> the next scores is a chain within an M tile, whose S and P share a place, and P goes over only when
+// all 128 columns are written.  No pipe is near its end: 1.2 instructions a cycle, XU 31 %, tensor 31 % (prompt of 2048).
+// With widening warps beside it (250 instructions a tile) the softmax by itself takes 3950, so where a sequence and head
+// has several units and many tiles, attention_widen_kernel writes the f16 tiles to the workspace once and this kernel copies them
+// (READY): a prompt of 8192 tokens, 28 / 4 heads, takes 500 us (0.96 PFLOP/s, 0.59 of what a large bf16 product reaches)
+// against 742, one of 2048, 32 / 8 heads, 71 against 82.  An item's end and the next one's start cost some 15000 cycles.
 // Tried without gain: sixteen softmax warps of 64 columns (registers: the scores have to be read twice; 10000 cycles a
 // tile), naps between two looks at a barrier, q of the next item brought early (1.7 % slower).
 //
-// Units go to the CTAs (one per SM) longest first, alternately up and down.  Where there are few, each is divided along
-// its tokens into as many parts as finish soonest; attention_wide_join_kernel adds the parts up in order.
+// Units go to the CTAs (one per SM) sequence by sequence, the longest of each first, alternately up and down.  Where there
+// are few, all are divided along their tokens into as many parts as let the longest finish soonest;
+// attention_wide_join_kernel adds the parts up in order.
 #pragma once
 #include <cstddef>
 #include <type_traits>

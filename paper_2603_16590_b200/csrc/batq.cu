@@ -1743,7 +1743,7 @@ bool plan_attention(const batq_kv_cache* c, int32_t q_heads, int64_t tokens, int
   if (a->narrow) {
     const int64_t rows = std::min<int64_t>(most, kNarrowRows);
     // As few units as can be, of 8, 16 or 24 rows (more of one do not fit the registers): 24 sequences of up to 20 rows
-    // one unit of 24 21.2 us, two of 16 22.3.  Beside prompts most of the others decode: 16.
+    // one unit of 24 21.2 us, two of 16 22.3.  Beside prompts 16 (not measured against others).
     a->nt = rows <= 8 ? 1 : !a->wide && (rows + 23) / 24 < (rows + 15) / 16 ? 3 : 2;
     const int64_t units = (rows + 8 * a->nt - 1) / (8 * a->nt) * c->kv_heads * batch;
     const int64_t tiles = std::max<int64_t>(1, (static_cast<int64_t>(max_kv) + kAtTile - 1) / kAtTile);
