@@ -316,8 +316,8 @@ batq_status batq_kv_cache_destroy(batq_kv_cache* c);
  *   keys     MXFP8(clip(rope(k) P_k)),  values  MXFP8(clip(v P_v))   to the token's slot,
  *   queries  bf16(rope(q) P_q)                                       to q_out,
  * in fp32 from the bf16 input to the one rounding.  Inputs are finite; a block with an infinity or NaN gets unspecified
- * codes, none of them NaN.  (Rows that do not see a token with a NaN come out as without it.  An infinity's scale is felt
- * by the keys it shares 128 tokens of a prompt's sequence with.)
+ * codes, none of them NaN.  (Rows that do not see a token with a NaN come out as without it, up to roundings.  An
+ * infinity's scale is felt by the keys it shares 128 tokens of a prompt's sequence with.)
  *   t_k, t_v, t_q  transforms with n = head_dim, or NULL (none); t_q as batq_transform_create_dual(t_k) makes it, with
  *                  no clip (else UNSUPPORTED).  UNSUPPORTED while one emulates bf16 intermediates.
  *   k, v           dev bf16 [tokens x kv_heads * head_dim], row strides ldk, ldv elements: e.g. column ranges of the
